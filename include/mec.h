@@ -306,6 +306,85 @@ int mec_conv2d_wgrad_noalloc(const void* I, const float* G, float* dK,
                              int k_h, int k_w, int k_c, int s_h, int s_w,
                              int dtype, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Layer operators: what stands next to the convolutions in a network, on the
+ * same activations and the same K. An n-h-w-c tensor is `rows` pixels (i_n*h*w)
+ * of its channels; consecutive pixels are `pitch` elements apart (the channel
+ * count, or more where the rows are a slice of a wider tensor's channels).
+ * `dtype` is the type of the activations, their gradients, K and dK; bias,
+ * gamma, beta, their gradients and the row statistics are fp32, and so is
+ * everything between: each output is rounded once. Widths and pitches go up to
+ * 2^20, rows to 2^30 (MEC_ERR_UNSUPPORTED beyond). Results are reproducible:
+ * every sum has an order fixed by the sizes and alignments (no atomics).
+ * Infinities and NaNs spread as in the formulas.
+ * ------------------------------------------------------------------------ */
+
+/* Activations: z; max(z, 0); z s(z); z s(2u), u = sqrt(2/pi) (z + 0.044715 z^3), the
+ * tanh form of GELU; with s(x) = 1 / (1 + e^-x). */
+enum mec_act { MEC_ACT_NONE = 0, MEC_ACT_RELU = 1, MEC_ACT_SILU = 2, MEC_ACT_GELU = 3 };
+
+/* A matrix product with bias, activation and residual in its epilogue, the 1x1
+ * convolution of every pixel:
+ *   z = X K + bias (+ R where residual_first),   Y = act(z) (+ R otherwise)
+ * X is rows x i_c, K i_c x k_c (dense), R and Y rows x k_c. bias and R may be
+ * NULL. Z, unless NULL, receives z (rows x k_c, dense, rounded to dtype) for the
+ * backward pass. R may be Y itself (then r_pitch = y_pitch); otherwise Y and Z
+ * must not overlap each other or the inputs.
+ * Returns MEC_OK or a negative status. */
+int mec_linear(const void* X, const void* K, const float* bias, const void* R, void* Y, void* Z,
+               int64_t rows, int i_c, int k_c, int64_t x_pitch, int64_t r_pitch, int64_t y_pitch,
+               int dtype, int act, int residual_first, void* stream);
+
+/* Its gradients, for G = dloss/dY (rows x k_c):
+ *   dZ = G act'(Z),  dX = dZ K^T,  dK = X^T dZ,  dbias = column sums of dZ
+ * from the Z that mec_linear left (relu'(z) = 1 for z > 0, else 0). The gradient of
+ * R is dZ where residual_first, else G. dZ and dX are dense, as Z is. dX, dK and
+ * dbias may each be NULL: not wanted (X is then read for dK, K for dX alone). With
+ * MEC_ACT_NONE dZ is G: Z and dZ may be NULL and are not touched; otherwise dZ is
+ * always written, and products take it as rounded to dtype; it may be Z's memory,
+ * or G's where g_pitch = k_c.
+ * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for the partial sums of
+ * dK and dbias; may be NULL where neither is wanted. */
+int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);
+int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX,
+                    void* dK, float* dbias, void* workspace, size_t workspace_bytes, int64_t rows,
+                    int i_c, int k_c, int64_t g_pitch, int64_t x_pitch, int dtype, int act, void* stream);
+
+/* Layer norm of every pixel's channels:
+ *   Y = (X - mean) rstd gamma + beta,  rstd = 1 / sqrt(mean((X - mean)^2) + eps), eps >= 0
+ * gamma (NULL: ones) and beta (NULL: zeros) have `channels` elements; mean and rstd
+ * (rows each), unless NULL, are kept for the backward pass. Y may be X itself (then
+ * y_pitch = x_pitch); otherwise they must not overlap. */
+int mec_layer_norm(const void* X, const float* gamma, const float* beta, void* Y, float* mean,
+                   float* rstd, int64_t rows, int channels, int64_t x_pitch, int64_t y_pitch,
+                   float eps, int dtype, void* stream);
+
+/* Its gradients, for G = dloss/dY, with xh = (X - mean) rstd and w = G gamma:
+ *   dX = rstd (w - mean(w) - xh mean(w xh)),  dgamma = sum over rows of G xh,
+ *   dbeta = sum over rows of G
+ * dX (rows x channels, dense), dgamma and dbeta may each be NULL: not wanted. dX must
+ * not overlap G or X. workspace: mec_layer_norm_grad_workspace_bytes, 4-byte aligned, for
+ * the partial sums of dgamma and dbeta; may be NULL where neither is wanted. */
+int64_t mec_layer_norm_grad_workspace_bytes(int64_t rows, int channels, int dtype);
+int mec_layer_norm_grad(const void* G, const void* X, const float* gamma, const float* mean,
+                        const float* rstd, void* dX, float* dgamma, float* dbeta, void* workspace,
+                        size_t workspace_bytes, int64_t rows, int channels, int64_t g_pitch,
+                        int64_t x_pitch, int dtype, void* stream);
+
+/* Newton-Schulz orthogonalisation of `batch` dense matrices U (rows x cols each), for an
+ * update of K from its gradient viewed as the (k_h*k_w*i_c) x k_c matrix:
+ *   X = U / (|U|_F + eps), then `steps` (1 to 100) times, with A = X X^T (rows <= cols):
+ *   X <- a X + (b A + c A^2) X      (else A = X^T X and X <- a X + X (b A + c A^2))
+ * O receives X. It drives every singular value s towards the fixed range of a s + b s^3 +
+ * c s^5: a = 3.4445, b = -4.7750, c = 2.0315 bring those above about 0.005 of |U|_F to
+ * 0.7 .. 1.2 in 5 steps. A zero matrix stays zero (eps > 0). O may be U itself.
+ * workspace: mec_orthogonalize_workspace_bytes, any alignment. batch <= 65535,
+ * rows, cols <= 2^20. */
+int64_t mec_orthogonalize_workspace_bytes(int batch, int rows, int cols, int dtype);
+int mec_orthogonalize(const void* U, void* O, void* workspace, size_t workspace_bytes, int batch,
+                      int rows, int cols, int steps, float a, float b, float c, float eps, int dtype,
+                      void* stream);
+
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* mec_strerror(int status);
 

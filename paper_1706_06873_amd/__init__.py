@@ -26,6 +26,8 @@ __all__ = [
     "GRAD_INPUT", "GRAD_KERNEL", "GRAD_KERNEL_FROM_L", "grad_workspace_bytes", "fold",
     "dgrad_gemm", "conv2d_dgrad", "wgrad_gemm", "conv2d_wgrad", "noalloc_scratch_bytes",
     "conv2d_wgrad_noalloc",
+    "linear", "linear_grad", "linear_grad_workspace_bytes", "layer_norm", "layer_norm_grad",
+    "layer_norm_grad_workspace_bytes", "orthogonalize", "orthogonalize_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -34,6 +36,7 @@ LIB_PATH = os.path.join(_HERE, "libmec.so")
 F32, BF16 = 0, 1
 LOWERED, FUSED, IM2COL = 0, 1, 2
 GRAD_INPUT, GRAD_KERNEL, GRAD_KERNEL_FROM_L = 0, 1, 2
+_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _ALGOS = {"lowered": LOWERED, "fused": FUSED, "im2col": IM2COL,
           LOWERED: LOWERED, FUSED: FUSED, IM2COL: IM2COL}
 
@@ -74,6 +77,19 @@ def _load(path):
     L.mec_noalloc_scratch_bytes.restype = ctypes.c_int64
     L.mec_conv2d_wgrad_noalloc.argtypes = [_vp, _vp, _vp] + _DIMS + [_i, _vp]
     L.mec_conv2d_wgrad_noalloc.restype = _i
+    i64, sz, f = ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+    L.mec_linear.argtypes = [_vp] * 6 + [i64, _i, _i, i64, i64, i64, _i, _i, _i, _vp]
+    L.mec_linear_grad_workspace_bytes.argtypes = [i64, _i, _i, _i]
+    L.mec_linear_grad.argtypes = [_vp] * 9 + [sz, i64, _i, _i, i64, i64, _i, _i, _vp]
+    L.mec_layer_norm.argtypes = [_vp] * 6 + [i64, _i, i64, i64, f, _i, _vp]
+    L.mec_layer_norm_grad_workspace_bytes.argtypes = [i64, _i, _i]
+    L.mec_layer_norm_grad.argtypes = [_vp] * 9 + [sz, i64, _i, i64, i64, _i, _vp]
+    L.mec_orthogonalize_workspace_bytes.argtypes = [_i] * 4
+    L.mec_orthogonalize.argtypes = [_vp] * 3 + [sz, _i, _i, _i, _i, f, f, f, f, _i, _vp]
+    for name in ("linear", "linear_grad", "layer_norm", "layer_norm_grad", "orthogonalize"):
+        getattr(L, "mec_" + name).restype = _i
+        if name not in ("linear", "layer_norm"):
+            getattr(L, "mec_%s_workspace_bytes" % name).restype = i64
     L.mec_strerror.argtypes = [_i]
     L.mec_strerror.restype = ctypes.c_char_p
     L.mec_last_error.argtypes = []
@@ -450,3 +466,232 @@ def conv2d_wgrad_noalloc(I, G, k_h, k_w, s_h=1, s_w=1, dK=None, stream=None):
                                         i_c, k_h, k_w, k_c, s_h, s_w, F32, _stream_handle(stream)),
            "mec_conv2d_wgrad_noalloc")
     return dK
+
+
+# ---------------------------------------------------------------- layer operators
+# What stands beside the convolutions in a network, on the same activations and the same K.
+# Activations are tensors with the channels last: contiguous, or 2-D (rows x channels) with
+# a row pitch, as a slice of a wider tensor's channels has. They, their gradients, K and dK
+# are float32 or bfloat16, all the same; bias, gamma, beta, their gradients and the row
+# statistics are float32.
+
+def _rows(t, name, width=None, dtype=None, ref=None):
+    """(rows, channels, pitch) of an activation."""
+    if t.dim() < 2:
+        raise ValueError("%s must have the channels as its last dimension and at least one more" % name)
+    c = t.shape[-1]
+    if width is not None and c != width:
+        raise ValueError("%s must have %d channels, got %d" % (name, width, c))
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if ref is not None:
+        _same_device(t, ref, name)
+    if t.is_contiguous():
+        return (t.numel() // c if c else 0), c, c
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= c:
+        return t.shape[0], c, t.stride(0)
+    raise ValueError("%s must be contiguous, or rows of contiguous channels" % name)
+
+
+def _ptr(t, name):
+    """The device pointer of an activation that _rows has checked, or None."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    return t.data_ptr()
+
+
+def _param(t, n, name, ref):
+    """The pointer of a float32 parameter vector of n elements, or None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or t.dtype != torch.float32:
+        raise ValueError("%s must be torch.float32 of shape %s, got %s of shape %s"
+                         % (name, (n,), t.dtype, tuple(t.shape)))
+    _same_device(t, ref, name)
+    return _dev_ptr(t, name)
+
+
+def _new(t, shape, dtype, ref, name):
+    """A given dense output, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=ref.device)
+    _check_out(t, shape, dtype, ref, name)
+    return t
+
+
+def _act_code(act):
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(sorted(_ACTS)), act))
+    return _ACTS[act]
+
+
+def _launch(name, ref, stream, *args):
+    """Calls an entry point on ref's device: the stream is its last argument."""
+    if ref.device.index != torch.cuda.current_device():
+        with torch.cuda.device(ref.device):
+            return _launch(name, ref, stream, *args)
+    if stream is None:
+        stream = torch.cuda.current_stream(ref.device)
+    _check(getattr(lib, name)(*args, stream.cuda_stream), name)
+
+
+def _matrix(K, name="K"):
+    """(i_c, k_c) of a kernel that acts on pixels: i_c x k_c, or 1 x 1 x i_c x k_c."""
+    if K.dim() == 4 and K.shape[0] == K.shape[1] == 1:
+        return K.shape[2], K.shape[3]
+    if K.dim() != 2:
+        raise ValueError("%s must be i_c x k_c, or 1 x 1 x i_c x k_c" % name)
+    return K.shape[0], K.shape[1]
+
+
+def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=None, Z=None, stream=None):
+    """Y = act(X K + bias) + residual, or act(X K + bias + residual) with residual_first, for
+    every pixel of X (... x i_c) and K of i_c x k_c (or 1 x 1 x i_c x k_c); act is "none",
+    "relu", "silu" or "gelu" (the tanh form). A given Z (Y's shape) receives act's argument,
+    for linear_grad. residual may be Y itself. Returns Y."""
+    i_c, k_c = _matrix(K)
+    dt = _dtype_code(X)
+    rows, _, x_pitch = _rows(X, "X", i_c)
+    if K.dtype != X.dtype:
+        raise TypeError("X and K must have the same dtype")
+    _same_device(K, X, "K")
+    a = _act_code(act)
+    shape = tuple(X.shape[:-1]) + (k_c,)
+    r_pitch = 0
+    if residual is not None:
+        if tuple(residual.shape) != shape:
+            raise ValueError("residual must be of shape %s, got %s" % (shape, tuple(residual.shape)))
+        r_pitch = _rows(residual, "residual", k_c, X.dtype, X)[2]
+    Y = _new(Y, shape, X.dtype, X, "Y")
+    y_pitch = _rows(Y, "Y")[2]
+    if Z is not None:
+        _check_out(Z, shape, X.dtype, X, "Z")
+    bias = _param(bias, k_c, "bias", X)
+    _launch("mec_linear", X, stream, _ptr(X, "X"), _dev_ptr(K, "K"), bias,
+            _ptr(residual, "residual"), _ptr(Y, "Y"), None if Z is None else _dev_ptr(Z, "Z"), rows, i_c, k_c,
+            x_pitch, r_pitch, y_pitch, dt, a, int(bool(residual_first)))
+    return Y
+
+
+def linear_grad_workspace_bytes(rows, i_c, k_c, dtype=F32):
+    return _check(lib.mec_linear_grad_workspace_bytes(rows, i_c, k_c, dtype), "mec_linear_grad_workspace_bytes")
+
+
+def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, dX=None, dK=None, dbias=None,
+                workspace=None, stream=None):
+    """Gradients of linear for G = dloss/dY: (dX, dK, dbias, dZ). Z is what linear left
+    (not needed with act "none"); `needs` says which of dX, dK and dbias are wanted, the
+    others come back as None (X may be None without dK). dZ, the gradient of act's argument, is G
+    itself with act "none"; the residual's gradient is dZ where it was added first, else G.
+    dK has K's dtype and shape, dbias is float32. A given workspace holds at least
+    linear_grad_workspace_bytes bytes."""
+    i_c, k_c = _matrix(K)
+    dt = _dtype_code(G)
+    rows, _, g_pitch = _rows(G, "G", k_c)
+    if K.dtype != G.dtype:
+        raise TypeError("G and K must have the same dtype")
+    _same_device(K, G, "K")
+    a = _act_code(act)
+    need_x, need_k, need_b = needs
+    x_pitch = i_c
+    if X is not None:
+        if tuple(X.shape[:-1]) != tuple(G.shape[:-1]):
+            raise ValueError("X and G must have the same pixels, got %s and %s" % (tuple(X.shape), tuple(G.shape)))
+        x_pitch = _rows(X, "X", i_c, G.dtype, G)[2]
+    elif need_k:
+        raise ValueError("X is needed for dK")
+    if a:
+        if Z is None:
+            raise ValueError("Z is needed with act %r" % act)
+        if tuple(Z.shape) != tuple(G.shape) or Z.dtype != G.dtype:
+            raise ValueError("Z must be %s of shape %s, got %s of shape %s"
+                             % (G.dtype, tuple(G.shape), Z.dtype, tuple(Z.shape)))
+        _same_device(Z, G, "Z")
+        dZ = _new(dZ, tuple(G.shape), G.dtype, G, "dZ")
+    dX = _new(dX, tuple(G.shape[:-1]) + (i_c,), G.dtype, G, "dX") if need_x else None
+    dK = _new(dK, tuple(K.shape), G.dtype, G, "dK") if need_k else None
+    dbias = _new(dbias, (k_c,), torch.float32, G, "dbias") if need_b else None
+    wp, wb = None, 0
+    if need_k or need_b:
+        need = linear_grad_workspace_bytes(rows, i_c, k_c, dt)
+        workspace, wp, wb = _given_workspace(need, workspace, G)
+    opt = lambda t, name: None if t is None else _dev_ptr(t, name)  # noqa: E731
+    _launch("mec_linear_grad", G, stream, _ptr(G, "G"), _ptr(X, "X"), _dev_ptr(K, "K"),
+            opt(Z, "Z") if a else None, opt(dZ, "dZ") if a else None, opt(dX, "dX"), opt(dK, "dK"),
+            opt(dbias, "dbias"), wp, wb, rows, i_c, k_c, g_pitch, x_pitch, dt, a)
+    return dX, dK, dbias, dZ if a else G
+
+
+def layer_norm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
+    """Layer norm of every pixel's channels, (X - mean) rstd gamma + beta with rstd =
+    1 / sqrt(variance + eps). Returns (Y, mean, rstd); mean and rstd (X's shape without the
+    channels, float32) are what layer_norm_grad takes. Y may be X itself."""
+    dt = _dtype_code(X)
+    rows, c, x_pitch = _rows(X, "X")
+    Y = _new(Y, tuple(X.shape), X.dtype, X, "Y")
+    y_pitch = _rows(Y, "Y")[2]
+    mean = _new(mean, tuple(X.shape[:-1]), torch.float32, X, "mean")
+    rstd = _new(rstd, tuple(X.shape[:-1]), torch.float32, X, "rstd")
+    gamma, beta = _param(gamma, c, "gamma", X), _param(beta, c, "beta", X)
+    _launch("mec_layer_norm", X, stream, _ptr(X, "X"), gamma, beta,
+            _ptr(Y, "Y"), _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), rows, c, x_pitch, y_pitch, eps, dt)
+    return Y, mean, rstd
+
+
+def layer_norm_grad_workspace_bytes(rows, channels, dtype=F32):
+    return _check(lib.mec_layer_norm_grad_workspace_bytes(rows, channels, dtype),
+                  "mec_layer_norm_grad_workspace_bytes")
+
+
+def layer_norm_grad(G, X, mean, rstd, gamma=None, needs=(True, True, True), dX=None, dgamma=None, dbeta=None,
+                    workspace=None, stream=None):
+    """Gradients of layer_norm for G = dloss/dY: (dX, dgamma, dbeta), of which `needs` says
+    which are wanted; the others come back as None. A given workspace holds at least
+    layer_norm_grad_workspace_bytes bytes."""
+    dt = _dtype_code(X)
+    rows, c, x_pitch = _rows(X, "X")
+    if tuple(G.shape) != tuple(X.shape):
+        raise ValueError("G must be of shape %s, got %s" % (tuple(X.shape), tuple(G.shape)))
+    g_pitch = _rows(G, "G", c, X.dtype, X)[2]
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _check_out(t, tuple(X.shape[:-1]), torch.float32, X, name)
+    if gamma is not None:
+        _check_out(gamma, (c,), torch.float32, X, "gamma")
+    dX = _new(dX, tuple(X.shape), X.dtype, X, "dX") if needs[0] else None
+    dgamma = _new(dgamma, (c,), torch.float32, X, "dgamma") if needs[1] else None
+    dbeta = _new(dbeta, (c,), torch.float32, X, "dbeta") if needs[2] else None
+    wp, wb = None, 0
+    if needs[1] or needs[2]:
+        workspace, wp, wb = _given_workspace(layer_norm_grad_workspace_bytes(rows, c, dt), workspace, X)
+    opt = lambda t, name: None if t is None else _dev_ptr(t, name)  # noqa: E731
+    _launch("mec_layer_norm_grad", X, stream, _ptr(G, "G"), _ptr(X, "X"), opt(gamma, "gamma"),
+            _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), opt(dX, "dX"), opt(dgamma, "dgamma"),
+            opt(dbeta, "dbeta"), wp, wb, rows, c, g_pitch, x_pitch, dt)
+    return dX, dgamma, dbeta
+
+
+def orthogonalize_workspace_bytes(batch, rows, cols, dtype=F32):
+    return _check(lib.mec_orthogonalize_workspace_bytes(batch, rows, cols, dtype),
+                  "mec_orthogonalize_workspace_bytes")
+
+
+def orthogonalize(U, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, O=None, workspace=None, stream=None):
+    """Newton-Schulz orthogonalisation of an update U, as float32 or bfloat16 matrices: one
+    (rows x cols) or a stack of them (batch x rows x cols), or one kernel's gradient
+    (k_h x k_w x i_c x k_c, taken as the (k_h*k_w*i_c) x k_c matrix) or a stack of those.
+    X = U / (|U|_F + eps), then X <- a X + (b A + c A^2) X with A = X X^T, `steps` times.
+    Returns O of U's shape; it may be U itself."""
+    dt = _dtype_code(U)
+    if U.dim() not in (2, 3, 4, 5):
+        raise ValueError("U must be a matrix, a kernel's gradient or a stack of either")
+    batch = U.shape[0] if U.dim() % 2 else 1
+    cols = U.shape[-1]
+    rows = U.numel() // (batch * cols) if batch * cols else 0
+    a, b, c = coefficients
+    O = _new(O, tuple(U.shape), U.dtype, U, "O")
+    workspace, wp, wb = _given_workspace(orthogonalize_workspace_bytes(batch, rows, cols, dt), workspace, U)
+    _launch("mec_orthogonalize", U, stream, _dev_ptr(U, "U"), _dev_ptr(O, "O"), wp, wb, batch, rows, cols, steps,
+            a, b, c, eps, dt)
+    return O

@@ -9,6 +9,7 @@
 #include <initializer_list>
 
 #include "mec_internal.h"
+#include "mec_product.h"
 
 namespace {
 
@@ -315,6 +316,212 @@ int mec_conv2d_wgrad(const void* I, const float* G, float* dK, void* workspace,
     // the products read L's rows straight from I: no lowering pass
     return hip_status(mec::launch_wgrad(s, static_cast<const float*>(I), G, part, dK, st, true),
                       "wgrad products from I");
+}
+
+// ---------------------------------------------------------------- layer operators
+
+namespace {
+
+// Widths and pitches that the kernels' 32-bit offsets within a tile hold, and rows that
+// their grids do.
+constexpr int64_t kMaxWidth = int64_t(1) << 20, kMaxRows = int64_t(1) << 30;
+
+// rows of `width` elements, `pitch` apart
+int check_rows(int64_t rows, int64_t width, int64_t pitch) {
+    if (rows < 1 || width < 1 || pitch < width) return MEC_ERR_INVALID_ARG;
+    if (rows > kMaxRows || pitch > kMaxWidth) return MEC_ERR_UNSUPPORTED;
+    return checked_product({rows, pitch}) < 0 ? MEC_ERR_INVALID_ARG : MEC_OK;
+}
+
+int first_error(std::initializer_list<int> codes) {
+    for (int c : codes)
+        if (c != MEC_OK) return c;
+    return MEC_OK;
+}
+
+bool valid_act(int act) { return act >= MEC_ACT_NONE && act <= MEC_ACT_GELU; }
+
+hipError_t launch_product(mec::Layout layout, const mec::Product& p, int dtype, hipStream_t st) {
+    return dtype == MEC_F32 ? mec::launch_product_f32(layout, p, st) : mec::launch_product_bf16(layout, p, st);
+}
+
+int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
+    const int64_t s = mec::product_splits(dtype, i_c, k_c, rows);
+    const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = mec::act_grad_shares(rows, k_c) * k_c * 4;
+    return dk > db ? dk : db;
+}
+
+}  // namespace
+
+int mec_linear(const void* X, const void* K, const float* bias, const void* R, void* Y, void* Z, int64_t rows, int i_c,
+               int k_c, int64_t x_pitch, int64_t r_pitch, int64_t y_pitch, int dtype, int act, int residual_first,
+               void* stream) {
+    const int rc = first_error({check_rows(rows, i_c, x_pitch), check_rows(rows, k_c, y_pitch),
+                                R ? check_rows(rows, k_c, r_pitch) : MEC_OK});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype) || !valid_act(act) || !X || !K || !Y) return MEC_ERR_INVALID_ARG;
+    const int64_t es = elem_bytes(dtype);
+    if (!aligned(X, es) || !aligned(K, es) || !aligned(bias, 4) || !aligned(R, es) || !aligned(Y, es) || !aligned(Z, es))
+        return MEC_ERR_ALIGNMENT;
+    mec::Product p{};
+    p.A = X;
+    p.B = K;
+    p.Y = Y;
+    p.Z = Z;
+    p.R = R;
+    p.bias = bias;
+    p.lda = x_pitch;
+    p.ldb = p.ldz = k_c;
+    p.ldr = r_pitch;
+    p.ldy = y_pitch;
+    p.M = (int32_t)rows;
+    p.N = k_c;
+    p.K = i_c;
+    p.act = act;
+    p.res_first = residual_first != 0;
+    p.alpha = p.beta = 1.0f;
+    p.splits = p.batch = 1;
+    clear_stale_error();
+    return hip_status(launch_product(mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
+}
+
+int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
+    const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
+    return linear_grad_bytes(rows, i_c, k_c, dtype);
+}
+
+int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX, void* dK, float* dbias,
+                    void* workspace, size_t workspace_bytes, int64_t rows, int i_c, int k_c, int64_t g_pitch,
+                    int64_t x_pitch, int dtype, int act, void* stream) {
+    int rc = first_error({check_rows(rows, k_c, g_pitch), X ? check_rows(rows, i_c, x_pitch) : check_rows(rows, i_c, i_c)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype) || !valid_act(act) || !G || (dX && !K) || (dK && !X) || (act != MEC_ACT_NONE && (!Z || !dZ)))
+        return MEC_ERR_INVALID_ARG;
+    const int64_t es = elem_bytes(dtype);
+    if (!aligned(G, es) || !aligned(X, es) || !aligned(K, es) || !aligned(Z, es) || !aligned(dZ, es) || !aligned(dX, es) ||
+        !aligned(dK, es) || !aligned(dbias, 4))
+        return MEC_ERR_ALIGNMENT;
+    if ((dK || dbias) && (!workspace || (uint64_t)workspace_bytes < (uint64_t)linear_grad_bytes(rows, i_c, k_c, dtype)))
+        return MEC_ERR_WORKSPACE;
+    if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
+    const hipStream_t st = (hipStream_t)stream;
+    float* const part = static_cast<float*>(workspace);
+    clear_stale_error();
+    if (act != MEC_ACT_NONE || dbias) {
+        rc = hip_status(mec::launch_act_grad(G, g_pitch, Z, act == MEC_ACT_NONE ? nullptr : dZ, dbias ? part : nullptr, rows,
+                                             k_c, act, dtype, st), "gradient of the activation");
+        if (rc == MEC_OK && dbias)
+            rc = hip_status(mec::launch_sum_parts(part, mec::act_grad_shares(rows, k_c), k_c, dbias, MEC_F32, st),
+                            "gradient of the bias");
+        if (rc != MEC_OK) return rc;
+    }
+    mec::Product p{};
+    p.alpha = 1.0f;
+    p.batch = p.splits = 1;
+    const void* const dz = act == MEC_ACT_NONE ? G : dZ;
+    const int64_t z_pitch = act == MEC_ACT_NONE ? g_pitch : k_c;
+    if (dX) {
+        p.A = dz;
+        p.lda = z_pitch;
+        p.B = K;
+        p.ldb = k_c;
+        p.Y = dX;
+        p.ldy = i_c;
+        p.M = (int32_t)rows;
+        p.N = i_c;
+        p.K = k_c;
+        rc = hip_status(launch_product(mec::Layout::kXKt, p, dtype, st), "gradient of the input");
+        if (rc != MEC_OK) return rc;
+    }
+    if (dK) {
+        p.A = X;
+        p.lda = x_pitch;
+        p.B = dz;
+        p.ldb = z_pitch;
+        p.Y = dK;
+        p.ldy = k_c;
+        p.M = i_c;
+        p.N = k_c;
+        p.K = (int32_t)rows;
+        p.splits = mec::product_splits(dtype, i_c, k_c, rows);
+        p.part = part;
+        rc = hip_status(launch_product(mec::Layout::kXtK, p, dtype, st), "gradient of the kernel");
+        if (rc == MEC_OK && p.splits > 1)
+            rc = hip_status(mec::launch_sum_parts(part, p.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
+    }
+    return rc;
+}
+
+int mec_layer_norm(const void* X, const float* gamma, const float* beta, void* Y, float* mean, float* rstd, int64_t rows,
+                   int channels, int64_t x_pitch, int64_t y_pitch, float eps, int dtype, void* stream) {
+    const int rc = first_error({check_rows(rows, channels, x_pitch), check_rows(rows, channels, y_pitch)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype) || !X || !Y || !(eps >= 0.0f)) return MEC_ERR_INVALID_ARG;
+    const int64_t es = elem_bytes(dtype);
+    if (!aligned(X, es) || !aligned(Y, es) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return MEC_ERR_ALIGNMENT;
+    clear_stale_error();
+    return hip_status(mec::launch_norm(X, x_pitch, gamma, beta, Y, y_pitch, mean, rstd, rows, channels, eps, dtype,
+                                       (hipStream_t)stream), "layer norm");
+}
+
+int64_t mec_layer_norm_grad_workspace_bytes(int64_t rows, int channels, int dtype) {
+    const int rc = check_rows(rows, channels, channels);
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
+    return mec::norm_grad_blocks(rows) * 2 * channels * 4;
+}
+
+int mec_layer_norm_grad(const void* G, const void* X, const float* gamma, const float* mean, const float* rstd, void* dX,
+                        float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, int64_t rows, int channels,
+                        int64_t g_pitch, int64_t x_pitch, int dtype, void* stream) {
+    const int rc = first_error({check_rows(rows, channels, g_pitch), check_rows(rows, channels, x_pitch)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype) || !G || !X || !mean || !rstd) return MEC_ERR_INVALID_ARG;
+    const int64_t es = elem_bytes(dtype);
+    if (!aligned(G, es) || !aligned(X, es) || !aligned(dX, es) || !aligned(gamma, 4) || !aligned(mean, 4) ||
+        !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4))
+        return MEC_ERR_ALIGNMENT;
+    if ((dgamma || dbeta) &&
+        (!workspace || (uint64_t)workspace_bytes < (uint64_t)mec_layer_norm_grad_workspace_bytes(rows, channels, dtype)))
+        return MEC_ERR_WORKSPACE;
+    if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
+    if (!dX && !dgamma && !dbeta) return MEC_OK;
+    clear_stale_error();
+    return hip_status(mec::launch_norm_grad(G, g_pitch, X, x_pitch, gamma, mean, rstd, dX, dgamma, dbeta,
+                                            static_cast<float*>(workspace), rows, channels, dtype, (hipStream_t)stream),
+                      "layer norm gradients");
+}
+
+namespace {
+
+int check_stack(int batch, int rows, int cols, int dtype) {
+    if (batch < 1 || rows < 1 || cols < 1 || !valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
+    if (batch > 65535 || rows > kMaxWidth || cols > kMaxWidth) return MEC_ERR_UNSUPPORTED;
+    return checked_product({batch, rows, cols}) < 0 ? MEC_ERR_INVALID_ARG : MEC_OK;
+}
+
+}  // namespace
+
+int64_t mec_orthogonalize_workspace_bytes(int batch, int rows, int cols, int dtype) {
+    const int rc = check_stack(batch, rows, cols, dtype);
+    return rc != MEC_OK ? rc : mec::orth_workspace_bytes(batch, rows, cols, dtype);
+}
+
+int mec_orthogonalize(const void* U, void* O, void* workspace, size_t workspace_bytes, int batch, int rows, int cols,
+                      int steps, float a, float b, float c, float eps, int dtype, void* stream) {
+    const int rc = check_stack(batch, rows, cols, dtype);
+    if (rc != MEC_OK) return rc;
+    if (!U || !O || steps < 1 || steps > 100 || !(eps >= 0.0f)) return MEC_ERR_INVALID_ARG;
+    const int64_t es = elem_bytes(dtype);
+    if (!aligned(U, es) || !aligned(O, es)) return MEC_ERR_ALIGNMENT;
+    if (!workspace || (uint64_t)workspace_bytes < (uint64_t)mec::orth_workspace_bytes(batch, rows, cols, dtype))
+        return MEC_ERR_WORKSPACE;
+    clear_stale_error();
+    return hip_status(mec::launch_orth(U, O, workspace, batch, rows, cols, steps, a, b, c, eps, dtype, (hipStream_t)stream),
+                      "orthogonalisation");
 }
 
 // ---------------------------------------------------------------- for the tests

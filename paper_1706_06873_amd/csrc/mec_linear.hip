@@ -1,0 +1,316 @@
+// bf16 matrix products of the layer operators (mec_product.h), on v_mfma_f32_32x32x16_bf16.
+//
+// A workgroup computes a tile of Y, 32*BM*WM x 32*BN*WN, from chunks of 64 of the reduction
+// in two stages of LDS: while one chunk's products run, the next is on its way. Operands are
+// staged as they are stored:
+//   stored along the reduction ([m][k], [n][k])  rows of 64 k, 128 bytes; granule g (8 k) of
+//     row r at g ^ (r & 7); a fragment (8 k of one row per lane) is one 16-byte read
+//   stored across it ([k][m], [k][n])  rows of one k; the 32-byte blocks (16 columns) of row
+//     k at block ^ (k & 7); a fragment is two transposing reads (ds_read_b64_tr_b16: 16
+//     lanes read 4 rows of 16 columns and each gets 4 k of one column)
+// Both orders put the lanes that read together on different banks. Rows of whole 16-byte
+// granules go straight to LDS (buffer_load .. lds; what lies past the end of the reduction
+// is past the resource's end and arrives as zeros); others go through registers, granules
+// cut off at the row's end element by element.
+#include "mec_product.h"
+
+namespace mec {
+namespace {
+
+constexpr int kKT = 64;  // chunk of the reduction
+
+template <int BM, int BN, int WM, int WN, Layout L, bool DMA>
+struct Cfg {
+    static constexpr int kBM = BM, kBN = BN, kWM = WM, kWN = WN;
+    static constexpr bool kAT = L == Layout::kXtK;   // A stored [k][m]
+    static constexpr bool kBT = L != Layout::kXKt;   // B stored [k][n]
+    static constexpr bool kDMA = DMA;
+    static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int AB = TM * kKT * 2, BB = TN * kKT * 2, STAGE = AB + BB;  // bytes
+    static constexpr int AI = TM * 8 / THREADS, BI = TN * 8 / THREADS;           // granules per thread
+    static constexpr int EPI = WAVES * 32 * (32 * BN + 4) * 4;
+    static constexpr int LDS = 2 * STAGE > EPI ? 2 * STAGE : EPI;
+    static_assert(TM * 8 % THREADS == 0 && TN * 8 % THREADS == 0 && LDS <= 160 * 1024, "tile");
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+__device__ inline uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ inline const char* scalar(const char* x) {
+    const uint64_t v = (uint64_t)x;
+    return (const char*)((uint64_t)scalar((uint32_t)(v >> 32)) << 32 | scalar((uint32_t)v));
+}
+
+// A raw buffer of `bytes` from `base` (both uniform), as the load's four scalar registers.
+__device__ inline u32x4v resource(const char* base, int64_t bytes) {
+    const uint64_t a = (uint64_t)base;
+    return u32x4v{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes > 0x7fffffff ? 0x7fffffffu : (uint32_t)bytes, 0x00027000u};
+}
+
+// 16 bytes per lane from the buffer at voff straight to LDS, at lds + 16 * lane; zeros from
+// past its end. The compiler does not see the load: the caller waits on vmcnt before the
+// data is read. M0 holds the LDS address; it cannot be declared clobbered and is put back.
+__device__ inline void to_lds16(u32x4v rsrc, uint32_t voff, uint32_t lds) {
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "s"(lds), "v"(voff), "s"(rsrc)
+        : "memory");
+}
+
+// 16 bytes at any 2-byte boundary
+__device__ inline u32x4v load_any(const uint16_t* src) {
+    struct __attribute__((packed, aligned(2))) Any {
+        u32x4v v;
+    };
+    return reinterpret_cast<const Any*>(src)->v;
+}
+__device__ inline u32x4v load_some(const uint16_t* src, int64_t have) {  // its first `have` elements, then zeros
+    if (have >= 8) return load_any(src);
+    u32x4v w = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < have) w[e / 2] |= (uint32_t)src[e] << (16 * (e % 2));
+    return w;
+}
+
+// One operand's T rows (stored along the reduction) or columns (TR: across it) of a tile.
+// WIDE items of 16 bytes per thread.
+template <int T, int THREADS, bool TR, bool DMA>
+struct Operand {
+    static constexpr int ITEMS = T * 8 / THREADS;
+    static constexpr int SW = T / 16 < 8 ? T / 16 - 1 : 7;
+    const char* base;   // uniform: the tile's first row and the chunk's first k
+    int64_t step;       // bytes from chunk to chunk
+    int64_t left;       // uniform: DMA, TR: bytes of rows from base on; else elements of the reduction from base on
+    int64_t ld;         // elements
+    uint32_t voff[TR && DMA ? 1 : ITEMS];
+    int32_t have;       // TR: columns from this thread's on; else 8 k of this thread's granule start here
+    int32_t k_at;       // else: first k of this thread's granule
+
+    // rows r0 .. of `count` rows (columns) of `ld` elements, reduction from k0 to k1
+    __device__ inline void init(const void* mem, int64_t ld_, int32_t r0, int32_t count, int64_t k0, int64_t k1, int tid) {
+        ld = ld_;
+        if constexpr (TR) {
+            const int pos = tid % (T / 8), k = tid / (T / 8);
+            const int col = (((pos >> 1) ^ (k & SW)) * 2 + (pos & 1)) * 8;
+            base = scalar(static_cast<const char*>(mem) + 2 * (k0 * ld + r0));
+            step = 2 * kKT * ld;
+            have = count - r0 - col;
+            k_at = k;
+            if constexpr (DMA) {
+                // columns past the last read the last 8 instead (count is a multiple of 8)
+                voff[0] = 2u * (uint32_t)(k * ld + (have > 0 ? col : count - r0 - 8));
+                left = 2 * ((k1 - k0) * ld - r0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) voff[i] = (uint32_t)(k + i * (THREADS * 8 / T));
+                k_at = col;
+                left = k1 - k0;
+            }
+        } else {
+            const int row = tid / 8, kg = (tid % 8) ^ (row & 7);
+            base = scalar(static_cast<const char*>(mem) + 2 * (r0 * ld + k0));
+            step = 2 * kKT;
+            left = k1 - k0;
+            k_at = 8 * kg;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                int r = row + i * (THREADS / 8);
+                if (r0 + r >= count) r = count - 1 - r0;  // rows past the last are not stored
+                voff[i] = DMA ? 2u * (uint32_t)(r * ld + 8 * kg) : (uint32_t)r;
+            }
+        }
+    }
+    __device__ inline void next() {
+        base += step;
+        left -= TR && DMA ? step : kKT;
+    }
+    // DMA: this chunk to LDS at `to`
+    __device__ inline void stage(uint32_t to, int wave) const {
+        if constexpr (TR) {
+            const u32x4v rs = resource(base, left > 0 ? left : 0);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                to_lds16(rs, voff[0] + (uint32_t)(i * (THREADS * 8 / T)) * 2u * (uint32_t)ld, to + (uint32_t)(i * THREADS + wave * 64) * 16u);
+        } else {
+            const u32x4v rs = resource(base, 0x7fffffff);
+            const bool past = k_at >= left;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                to_lds16(rs, past ? 0x80000000u : voff[i], to + (uint32_t)(i * THREADS + wave * 64) * 16u);
+        }
+    }
+    // else: this chunk to registers, and from there to LDS
+    __device__ inline void load(u32x4v* r) const {
+        const uint16_t* const src = reinterpret_cast<const uint16_t*>(base);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if constexpr (TR)
+                r[i] = voff[i] < left ? load_some(src + voff[i] * ld + k_at, have) : u32x4v{0, 0, 0, 0};
+            else
+                r[i] = load_some(src + voff[i] * ld + k_at, left - k_at);
+        }
+    }
+    static __device__ inline void put(const u32x4v* r, char* to, int tid) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) *reinterpret_cast<u32x4v*>(to + (i * THREADS + tid) * 16) = r[i];
+    }
+    // the fragment of 32-row block blk for the 16 k from 16*kk on
+    static __device__ inline bf16x8 frag(const char* from, int blk, int kk, int lane) {
+        if constexpr (TR) {
+            const int p = lane & 15, c16 = blk * 2 + ((lane >> 4) & 1);
+            s16x4 h[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int k = kk * 16 + 8 * (lane >> 5) + 4 * s + (p >> 2);
+                const char* const at = from + k * (T * 2) + ((c16 ^ (k & SW)) << 5) + (p & 3) * 8;
+                h[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)at);
+            }
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int r = blk * 32 + (lane & 31), g = 2 * kk + (lane >> 5);
+            return *reinterpret_cast<const bf16x8*>(from + r * 128 + ((g ^ (r & 7)) << 4));
+        }
+    }
+};
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
+    constexpr int BM = C::kBM, BN = C::kBN;
+    using OpA = Operand<C::TM, C::THREADS, C::kAT, C::kDMA>;
+    using OpB = Operand<C::TN, C::THREADS, C::kBT, C::kDMA>;
+    __shared__ __align__(16) char lds[C::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = (int)scalar((uint32_t)tid >> 6);
+    const int wm = wave % C::kWM, wn = wave / C::kWM;
+    const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    const uint32_t split = b / tiles;
+    uint32_t mt, nt;
+    tile_of(b - split * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
+    const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
+    const int64_t k0 = (int64_t)split * p.chunks * kKT;
+    const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
+    const int chunks = (int)((k1 - k0 + kKT - 1) / kKT);
+
+    OpA a;
+    OpB bb;
+    a.init(p.A, p.lda, m0, p.M, k0, k1, tid);
+    bb.init(p.B, p.ldb, n0, p.N, k0, k1, tid);
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_char*)lds;
+
+    floatx16 acc[BM][BN] = {};
+    auto products = [&](const char* from) {
+#pragma unroll
+        for (int kk = 0; kk < kKT / 16; ++kk) {
+            bf16x8 fa[BM], fb[BN];
+#pragma unroll
+            for (int i = 0; i < BM; ++i) fa[i] = OpA::frag(from, wm * BM + i, kk, lane);
+#pragma unroll
+            for (int j = 0; j < BN; ++j) fb[j] = OpB::frag(from + C::AB, wn * BN + j, kk, lane);
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+#pragma unroll
+                for (int j = 0; j < BN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        }
+    };
+    if constexpr (C::kDMA) {
+        a.stage(at, wave);
+        bb.stage(at + C::AB, wave);
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t now = (c & 1) * C::STAGE, then = C::STAGE - now;
+            // this chunk has arrived for every wave, and none reads the other stage any more
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (c + 1 < chunks) {
+                a.next();
+                bb.next();
+                a.stage(at + then, wave);
+                bb.stage(at + then + C::AB, wave);
+            }
+            products(lds + now);
+        }
+    } else {
+        u32x4v ra[OpA::ITEMS], rb[OpB::ITEMS];
+        a.load(ra);
+        bb.load(rb);
+        OpA::put(ra, lds, tid);
+        OpB::put(rb, lds + C::AB, tid);
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t now = (c & 1) * C::STAGE, then = C::STAGE - now;
+            __syncthreads();
+            const bool more = c + 1 < chunks;
+            if (more) {
+                a.next();
+                bb.next();
+                a.load(ra);
+                bb.load(rb);
+            }
+            products(lds + now);
+            if (more) {
+                OpA::put(ra, lds + then, tid);
+                OpB::put(rb, lds + then + C::AB, tid);
+            }
+        }
+    }
+    __syncthreads();
+    float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * (32 * BN + 4);
+    epilogue<uint16_t, BM, BN>(p, acc, mine, m0 + wm * BM * 32, n0 + wn * BN * 32, 0, (int32_t)split, lane);
+}
+
+template <int BM, int BN, int WM, int WN, Layout L>
+hipError_t run(Product p, hipStream_t stream) {
+    using C = Cfg<BM, BN, WM, WN, L, true>;
+    p.m_tiles = (p.M + C::TM - 1) / C::TM;
+    p.n_tiles = (p.N + C::TN - 1) / C::TN;
+    const int64_t chunks = ((int64_t)p.K + kKT - 1) / kKT;
+    p.chunks = (int32_t)((chunks + p.splits - 1) / p.splits);
+    const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * p.splits;
+    if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
+    if (p.clean) {
+        hipLaunchKernelGGL(product_bf16_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
+    } else {
+        using G = Cfg<BM, BN, WM, WN, L, false>;
+        hipLaunchKernelGGL(product_bf16_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+template <Layout L>
+hipError_t pick(const Product& p, hipStream_t stream) {
+    return run<2, 2, 2, 2, L>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_product_bf16(Layout layout, Product p, hipStream_t stream) {
+    auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 8 == 0); };
+    p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0;
+    // the dimension that each operand's rows run along has to be whole granules
+    const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
+    p.clean = rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;
+    switch (layout) {
+        case Layout::kXK: return pick<Layout::kXK>(p, stream);
+        case Layout::kXKt: return pick<Layout::kXKt>(p, stream);
+        default: return pick<Layout::kXtK>(p, stream);
+    }
+}
+
+// Shares of the reduction: as many as fill 512 workgroups of the products' 128-wide tiles,
+// with at least 512 elements of the reduction each and none empty.
+int32_t product_splits(int, int64_t M, int64_t N, int64_t K) {
+    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), chunks = (K + kKT - 1) / kKT;
+    int64_t s = 512 / tiles;
+    if (s > chunks / 8) s = chunks / 8;
+    if (s > 64) s = 64;
+    if (s < 2) return 1;
+    const int64_t per = (chunks + s - 1) / s;
+    return (int32_t)((chunks + per - 1) / per);
+}
+
+}  // namespace mec

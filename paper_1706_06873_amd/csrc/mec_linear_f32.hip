@@ -1,0 +1,283 @@
+// fp32 matrix products of the layer operators (mec_product.h) on the bf16 matrix cores: each
+// operand value is split without loss into three bf16 values and a product is six bf16
+// products (mec_gemm_tile.hip says how exact that is, and mec_split.h what happens to values
+// that the split does not hold). A workgroup computes a tile of Y, 32*BM*WM x 32*BN*WN, from
+// chunks of 32 of the reduction in two stages of LDS; chunks travel through registers, where
+// they are split.
+#include "mec_product.h"
+#include "mec_split.h"
+
+namespace mec {
+namespace {
+
+constexpr int kKT = 32, kG = kKT / 8;  // chunk of the reduction, groups of 8 in it
+
+// TAIL: an operand stored along the reduction ends inside a group of 8.
+template <int BM, int BN, int WM, int WN, Layout L, bool TAIL>
+struct Cfg {
+    static constexpr int kBM = BM, kBN = BN, kWM = WM, kWN = WN;
+    static constexpr bool kAT = L == Layout::kXtK, kBT = L != Layout::kXKt;  // stored across the reduction
+    static constexpr bool kTail = TAIL;
+    static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int APL = TM * kKT * 2, BPL = TN * kKT * 2, STAGE = 3 * (APL + BPL);  // bytes (of a plane)
+    static constexpr int EPI = WAVES * 32 * (32 * BN + 4) * 4;
+    static constexpr int LDS = 2 * STAGE > EPI ? 2 * STAGE : EPI;
+    static constexpr int kPerSimd = WAVES == 8 ? 2 : (LDS <= 80 * 1024 ? 2 : 1);
+    static_assert(TM * kG % THREADS == 0 && TN * kG % THREADS == 0 && THREADS % TM == 0 && THREADS % TN == 0 && LDS <= 158 * 1024, "tile");
+};
+
+// One operand's T rows (stored along the reduction) or columns (TR: across it) of a tile.
+template <int T, int THREADS, bool TR, bool TAIL>
+struct Operand {
+    static constexpr int ITEMS = T * kG / THREADS;
+    const char* base;  // uniform: the tile's first row and the chunk's first k
+    int64_t bytes;     // uniform: from base to the end of what may be read
+    int64_t step;      // bytes from chunk to chunk
+    int32_t left;      // elements of the reduction from base on
+    uint32_t voff[TR ? 8 : ITEMS];
+    uint32_t pitch;    // TR: bytes between the groups of two items
+    uint32_t lds[ITEMS];
+    int32_t k_at;      // first k of this thread's group in a chunk
+
+    __device__ inline void init(const void* mem, int64_t ld, int32_t r0, int32_t count, int64_t k0, int64_t k1, int tid) {
+        left = (int32_t)(k1 - k0);
+        if constexpr (TR) {
+            const int col = tid % T, g = __builtin_amdgcn_readfirstlane(tid / T);
+            base = uniform(static_cast<const char*>(mem) + 4 * (k0 * ld + r0));
+            bytes = 4 * ((int64_t)left * ld - r0);  // rows past k1 lie past it
+            step = 4 * kKT * ld;
+            pitch = (uint32_t)(THREADS / T) * 32u * (uint32_t)ld;
+            const int c = r0 + col < count ? col : count - 1 - r0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) voff[e] = 4u * (uint32_t)((g * 8 + e) * ld + c);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) lds[i] = swz((uint32_t)col, (uint32_t)(g + i * (THREADS / T)));
+        } else {
+            const int g = tid % kG, row = tid / kG;
+            base = uniform(static_cast<const char*>(mem) + 4 * (r0 * ld + k0));
+            bytes = 4 * ((int64_t)(count - 1 - r0) * ld + left);
+            step = 4 * kKT;
+            k_at = 8 * g;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                int r = row + i * (THREADS / kG);
+                lds[i] = swz((uint32_t)r, (uint32_t)g);
+                if (r0 + r >= count) r = count - 1 - r0;  // rows past the last are not stored
+                voff[i] = 4u * (uint32_t)(r * ld + 8 * g);
+            }
+        }
+    }
+    // this chunk to registers, and on to the next. k past the last come as zeros.
+    __device__ inline void load(float (*x)[8]) {
+        const __amdgpu_buffer_rsrc_t rs = buffer(base, bytes > 0x7fffffff ? 0x7fffffff : bytes > 0 ? (int)bytes : 0);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if constexpr (TR) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[i][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, voff[e] + i * pitch, 0, 0));
+            } else {
+                load8(rs, k_at < left ? voff[i] : 0x80000000u, x[i]);
+                if constexpr (TAIL) {
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) x[i][e] = k_at + e < left ? x[i][e] : 0.0f;
+                }
+            }
+        }
+        base += step;
+        bytes -= step;
+        left -= kKT;
+    }
+    __device__ inline void put(const float (*x)[8], char* __restrict__ to, uint32_t& lost) const {
+        constexpr int PL = T * kKT * 2;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            u32x4 h, m, l;
+            split8(x[i], h, m, l, lost);
+            *reinterpret_cast<u32x4*>(to + lds[i]) = h;
+            *reinterpret_cast<u32x4*>(to + PL + lds[i]) = m;
+            *reinterpret_cast<u32x4*>(to + 2 * PL + lds[i]) = l;
+        }
+    }
+};
+
+// A 32 x 32 block in plain fp32, for values that the split does not hold: this lane's row of
+// A and column of B, with their elements a_k and b_k apart.
+__device__ __attribute__((noinline)) floatx16 plain_block(const float* a, int64_t a_k, const float* b, int64_t b_k, int32_t K, int lane) {
+    floatx16 sum = {};
+    auto fetch = [&](const float* from, int64_t ks, uint32_t s, float* x) {
+        const int32_t k = (int32_t)(s * 16u) + 8 * (lane >> 5);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e < K ? from[(k + e) * ks] : 0.0f;
+    };
+    plain_products(
+        sum, ((uint32_t)K + 15u) / 16u, [&](uint32_t s, float* x) { fetch(b, b_k, s, x); },
+        [&](uint32_t s, float* x) { fetch(a, a_k, s, x); });
+    return sum;
+}
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Product p) {
+    constexpr int BM = C::kBM, BN = C::kBN;
+    using OpA = Operand<C::TM, C::THREADS, C::kAT, C::kTail>;
+    using OpB = Operand<C::TN, C::THREADS, C::kBT, C::kTail>;
+    __shared__ __align__(16) char lds[C::LDS];
+    __shared__ uint32_t lost_s;  // some thread's split left bits out
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave % C::kWM, wn = wave / C::kWM;
+    const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    const uint32_t share = b / tiles;  // of the reduction, or which product of a batch
+    const int32_t split = p.splits > 1 ? (int32_t)share : 0, bat = p.splits > 1 ? 0 : (int32_t)share;
+    uint32_t mt, nt;
+    tile_of(b - share * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
+    const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
+    const int64_t k0 = (int64_t)split * p.chunks * kKT;
+    const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
+    const int chunks = (int)((k1 - k0 + kKT - 1) / kKT);
+    const float* const A = static_cast<const float*>(p.A) + bat * p.a_batch;
+    const float* const B = static_cast<const float*>(p.B) + bat * p.b_batch;
+
+    if (tid == 0) lost_s = 0;  // (ordered by the first barriers)
+    OpA oa;
+    OpB ob;
+    oa.init(A, p.lda, m0, p.M, k0, k1, tid);
+    ob.init(B, p.ldb, n0, p.N, k0, k1, tid);
+    struct Regs {
+        float a[OpA::ITEMS][8], b[OpB::ITEMS][8];
+    };
+    uint32_t lost = 0;
+    auto load = [&](Regs& r) {
+        oa.load(r.a);
+        ob.load(r.b);
+    };
+    auto stage = [&](const Regs& r, char* __restrict__ to) {
+        oa.put(r.a, to, lost);
+        ob.put(r.b, to + 3 * C::APL, lost);
+    };
+    floatx16 acc[BM][BN] = {}, low[BM][BN] = {};
+    struct Frags {
+        bf16x8 a[BM][3], b[BN][3];
+    };
+    auto read = [&](Frags& f, const char* __restrict__ from, int kk) {
+        const uint32_t g = (uint32_t)(2 * kk + (lane >> 5));
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+                f.a[i][q] = *reinterpret_cast<const bf16x8*>(from + q * C::APL + swz((uint32_t)((wm * BM + i) * 32 + (lane & 31)), g));
+#pragma unroll
+            for (int j = 0; j < BN; ++j)
+                f.b[j][q] = *reinterpret_cast<const bf16x8*>(from + 3 * C::APL + q * C::BPL + swz((uint32_t)((wn * BN + j) * 32 + (lane & 31)), g));
+        }
+    };
+    // B's columns are the instruction's rows (see the epilogue)
+    auto products = [&](const Frags& f) {
+#define MEC_MM(X, Y, ACC)                              \
+    _Pragma("unroll") for (int i = 0; i < BM; ++i)     \
+        _Pragma("unroll") for (int j = 0; j < BN; ++j) \
+            ACC[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[j][Y], f.a[i][X], ACC[i][j], 0, 0, 0);
+        MEC_MM(0, 0, acc)
+        MEC_MM(1, 0, low)
+        MEC_MM(0, 1, low)
+        MEC_MM(1, 1, low)
+        MEC_MM(2, 0, low)
+        MEC_MM(0, 2, low)
+#undef MEC_MM
+    };
+    // one chunk at a time in registers: it is requested while the first half of the chunk
+    // before the last is multiplied, and split into the other stage a chunk later
+    Frags f;
+    Regs r;
+    load(r);
+    stage(r, lds);
+    load(r);
+    __syncthreads();
+    auto step = [&](const char* __restrict__ cur, char* __restrict__ nxt) {
+        read(f, cur, 0);
+        stage(r, nxt);
+        products(f);
+        read(f, cur, 1);
+        load(r);
+        products(f);
+        __syncthreads();
+    };
+    for (int c = 0; c < chunks; c += 2) {  // (chunks past the last are zeros)
+        step(lds, lds + C::STAGE);
+        step(lds + C::STAGE, lds);
+    }
+
+    // Values the split does not hold. Rows and columns past the last are copies of the
+    // last, so all accumulators count.
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+        for (int j = 0; j < BN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float x = acc[i][j][v] + low[i][j][v];
+                acc[i][j][v] = x;
+                const uint32_t bits = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+                most = bits > most ? bits : most;
+            }
+    if (lost & 0xffffu) lost_s = 1;
+    __syncthreads();
+    float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * (32 * BN + 4);
+    const int32_t mw = m0 + wm * BM * 32, nw = n0 + wn * BN * 32;
+    if (lost_s || __any(most >= 0x7f800000u)) {
+        const int64_t ars = C::kAT ? 1 : p.lda, aks = C::kAT ? p.lda : 1;
+        const int64_t brs = C::kBT ? 1 : p.ldb, bks = C::kBT ? p.ldb : 1;
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) {
+                int32_t m = mw + i * 32 + (lane & 31), n = nw + j * 32 + (lane & 31);
+                m = m < p.M ? m : p.M - 1;
+                n = n < p.N ? n : p.N - 1;
+                acc[i][j] = plain_block(A + m * ars + k0 * aks, aks, B + n * brs + k0 * bks, bks, (int32_t)(k1 - k0), lane);
+            }
+    }
+    epilogue<float, BM, BN>(p, acc, mine, mw, nw, bat, split, lane);
+}
+
+template <int BM, int BN, int WM, int WN, Layout L>
+hipError_t run(Product p, hipStream_t stream) {
+    using C = Cfg<BM, BN, WM, WN, L, false>;
+    p.m_tiles = (p.M + C::TM - 1) / C::TM;
+    p.n_tiles = (p.N + C::TN - 1) / C::TN;
+    // shares are whole multiples of 64 elements, as product_splits counts them
+    const int64_t chunks = 2 * (((int64_t)p.K + 63) / 64);
+    p.chunks = 2 * (int32_t)((chunks / 2 + p.splits - 1) / p.splits);
+    const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * (p.splits > 1 ? p.splits : p.batch);
+    if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
+    if constexpr (L != Layout::kXtK) {
+        if (p.K % 8) {
+            using G = Cfg<BM, BN, WM, WN, L, true>;
+            hipLaunchKernelGGL(product_f32_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL(product_f32_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <Layout L>
+hipError_t pick(const Product& p, hipStream_t stream) {
+    return run<1, 2, 4, 1, L>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_product_f32(Layout layout, Product p, hipStream_t stream) {
+    auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 4 == 0); };
+    p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0 &&
+            p.y_batch % 4 == 0 && p.r_batch % 4 == 0;
+    switch (layout) {
+        case Layout::kXK: return pick<Layout::kXK>(p, stream);
+        case Layout::kXKt: return pick<Layout::kXKt>(p, stream);
+        default: return pick<Layout::kXtK>(p, stream);
+    }
+}
+
+}  // namespace mec

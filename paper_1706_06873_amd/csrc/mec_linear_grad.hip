@@ -1,0 +1,186 @@
+// What the gradients of the layer operators need beside their products: dZ = G act'(Z) with
+// the column sums of dZ, and the sums of partial sums.
+//
+// act_grad_kernel is one pass over G and Z, bound by memory. A workgroup takes a strip of
+// columns and a share of the rows; a thread keeps the sums of its own columns in registers
+// over all of its rows, the workgroup joins them in LDS and writes one row of partial sums,
+// and sum_parts adds those in a fixed order: no atomics, the same bits every time.
+#include "mec_product.h"
+
+namespace mec {
+namespace {
+
+struct ActGradParams {
+    const void* G;
+    const void* Z;
+    void* dZ;     // or nullptr (then act is none)
+    float* part;  // shares x N, or nullptr
+    int64_t ldg, rows, rows_per_share;
+    int32_t N, act;
+};
+
+// V columns per thread, TX threads across the columns, 256 / TX rows at a time.
+template <class E, int V, int TX>
+__global__ __launch_bounds__(256) void act_grad_kernel(ActGradParams p) {
+    constexpr int TY = 256 / TX;
+    constexpr bool FAST = sizeof(E) == 2;
+    __shared__ float sums[TY > 1 ? 256 * V : 1];
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+    const int32_t n = (int32_t)(blockIdx.x * TX + tx) * V;
+    const int64_t r0 = (int64_t)blockIdx.y * p.rows_per_share;
+    const int64_t r1 = r0 + p.rows_per_share < p.rows ? r0 + p.rows_per_share : p.rows;
+    float sum[V] = {};
+    if (n < p.N) {
+        for (int64_t r = r0 + ty; r < r1; r += TY) {
+            const E* const g = static_cast<const E*>(p.G) + r * p.ldg + n;
+            float x[V];
+            if constexpr (V == 8) load8v(g, x); else x[0] = to_float(g[0]);
+            if (p.act != kActNone) {
+                const E* const at = static_cast<const E*>(p.Z) + r * p.N + n;
+                float z[V];
+                if constexpr (V == 8) load8v(at, z); else z[0] = to_float(at[0]);
+                if (p.act == kActRelu) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) x[e] = z[e] > 0.0f ? x[e] : 0.0f;
+                } else if (p.act == kActSilu) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) x[e] *= act_slope<FAST>(kActSilu, z[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) x[e] *= act_slope<FAST>(kActGelu, z[e]);
+                }
+            }
+            if (p.dZ) {
+                E* const to = static_cast<E*>(p.dZ) + r * p.N + n;
+                if constexpr (V == 8) store8v(to, x); else to[0] = from_float<E>(x[0]);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += x[e];
+        }
+    }
+    if (!p.part) return;  // (the same for every thread)
+    if constexpr (TY > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[(ty * TX + tx) * V + e] = sum[e];
+        __syncthreads();
+        if (ty) return;
+#pragma unroll
+        for (int y = 1; y < TY; ++y)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += sums[(y * TX + tx) * V + e];
+    }
+    if (n < p.N)
+#pragma unroll
+        for (int e = 0; e < V; ++e) p.part[(int64_t)blockIdx.y * p.N + n + e] = sum[e];
+}
+
+// Partial sums part[i*n + j], i < count: output j < n0 goes to out[j], the others to
+// out2[j - n0]; either may be nullptr.
+template <class E>
+struct SumParams {
+    const float* part;
+    E* out;
+    E* out2;
+    int64_t n, n0;
+    int32_t count;
+    __device__ inline void put(int64_t j, float s) const {
+        if (j < n0) {
+            if (out) out[j] = from_float<E>(s);
+        } else if (out2) {
+            out2[j - n0] = from_float<E>(s);
+        }
+    }
+};
+
+// One output per thread, count partial sums one after another.
+template <class E>
+__global__ __launch_bounds__(256) void sum_few_kernel(SumParams<E> p) {
+    for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < p.n; j += (int64_t)gridDim.x * 256) {
+        float s = 0.0f;
+#pragma unroll 4
+        for (int32_t i = 0; i < p.count; ++i) s += p.part[i * p.n + j];
+        p.put(j, s);
+    }
+}
+
+// 64 outputs per workgroup: 16 waves take every 16th partial sum, then join.
+template <class E>
+__global__ __launch_bounds__(1024) void sum_many_kernel(SumParams<E> p) {
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (j < p.n)
+#pragma unroll 8
+        for (int32_t i = wave; i < p.count; i += 16) s += p.part[i * p.n + j];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave || j >= p.n) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    p.put(j, s);
+}
+
+template <class E>
+hipError_t sum_parts(const float* part, int64_t count, int64_t n, int64_t n0, void* out, void* out2, hipStream_t stream) {
+    SumParams<E> p{part, static_cast<E*>(out), static_cast<E*>(out2), n, n0, (int32_t)count};
+    if (count <= 32 || n > (int64_t(1) << 20)) {
+        const int64_t blocks = (n + 255) / 256;
+        hipLaunchKernelGGL(sum_few_kernel<E>, dim3((uint32_t)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream, p);
+    } else {
+        hipLaunchKernelGGL(sum_many_kernel<E>, dim3((uint32_t)((n + 63) / 64)), dim3(1024), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+template <class E, int V, int TX>
+hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
+    const uint32_t strips = (uint32_t)((p.N + V * TX - 1) / (V * TX));
+    hipLaunchKernelGGL((act_grad_kernel<E, V, TX>), dim3(strips, shares), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <class E>
+hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
+    constexpr int64_t W = 16 / sizeof(E);
+    const bool vec = p.N % 8 == 0 && p.ldg % W == 0 && !(((uintptr_t)p.G | (uintptr_t)p.Z | (uintptr_t)p.dZ) & 15u);
+    if (!vec) return p.N > 64 ? act_grad<E, 1, 256>(p, shares, stream) : act_grad<E, 1, 64>(p, shares, stream);
+    return p.N > 512 ? act_grad<E, 8, 128>(p, shares, stream)
+                     : p.N > 128 ? act_grad<E, 8, 32>(p, shares, stream) : act_grad<E, 8, 16>(p, shares, stream);
+}
+
+}  // namespace
+
+hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* out, int dtype, hipStream_t stream) {
+    return dtype ? sum_parts<uint16_t>(part, count, n, n, out, nullptr, stream)
+                 : sum_parts<float>(part, count, n, n, out, nullptr, stream);
+}
+hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* out, float* out2, hipStream_t stream) {
+    return sum_parts<float>(part, count, 2 * n, n, out, out2, stream);
+}
+
+// Shares of the rows: enough to fill the GPU, at least 32 rows each, and partial sums that
+// stay a small part of the traffic.
+int32_t act_grad_shares(int64_t rows, int64_t N) {
+    const int64_t strips = (N + 511) / 512;
+    int64_t shares = (rows + 31) / 32, most = 2048 / strips > 1 ? 2048 / strips : 1;
+    return (int32_t)(shares < most ? shares : most);
+}
+
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* part, int64_t rows, int32_t N, int act,
+                           int dtype, hipStream_t stream) {
+    const int32_t shares = act_grad_shares(rows, N);
+    ActGradParams p{};
+    p.G = G;
+    p.Z = Z;
+    p.dZ = dZ;
+    p.part = part;
+    p.ldg = ldg;
+    p.rows = rows;
+    p.rows_per_share = (rows + shares - 1) / shares;
+    p.N = N;
+    p.act = act;
+    return dtype ? act_grad<uint16_t>(p, (uint32_t)shares, stream) : act_grad<float>(p, (uint32_t)shares, stream);
+}
+
+}  // namespace mec

@@ -1,0 +1,259 @@
+// Matrix products of the layer operators (mec_linear.hip in bf16, mec_linear_f32.hip in
+// fp32): what they compute, and the epilogue that both share.
+//
+//   acc = A B, then per output (m, n), all in fp32:
+//   z = alpha*acc + bias[n] (+ beta*R[m, n] with res_first),  Z = z,
+//   Y = act(z) (+ beta*R[m, n] without it)
+//
+// A is M x K, stored [m][k] or [k][m]; B is K x N, stored [n][k] or [k][n]: the layouts of
+// Y = X K ([m][k], [k][n]), dX = dZ K^T ([m][k], [n][k]) and dK = X^T dZ ([k][m], [k][n]).
+#pragma once
+
+#include <stdint.h>
+
+#include "mec_internal.h"
+
+namespace mec {
+
+enum class Layout { kXK = 0, kXKt = 1, kXtK = 2 };  // the three above
+
+enum Act { kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3 };
+
+struct Product {
+    const void* A;
+    const void* B;
+    void* Y;
+    void* Z;         // or nullptr
+    const void* R;   // or nullptr
+    const float* bias;  // or nullptr
+    float* part;     // with splits > 1: splits x M x N partial sums in place of Y
+    int64_t lda, ldb, ldy, ldz, ldr;  // elements per row as stored
+    int32_t M, N, K;
+    int32_t act, res_first;
+    float alpha, beta;
+    int32_t splits;  // of the reduction
+    int32_t batch;   // equal products, the strides below apart (elements)
+    int64_t a_batch, b_batch, y_batch, r_batch;
+    int32_t symmetric;  // Y is square and symmetric (A A^T): tiles above the diagonal are mirrored
+
+    // filled by the launch
+    int32_t m_tiles, n_tiles, chunks;  // chunks of the reduction per split
+    int32_t vec;                       // 16-byte rows of Y, Z and R, 16-byte partial sums
+    int32_t clean;                     // 16-byte rows of A and B
+};
+
+// Enqueue the product; A, B, Z, R, Y bf16 or fp32. splits > 1 leaves the partial sums.
+hipError_t launch_product_bf16(Layout layout, Product p, hipStream_t stream);
+hipError_t launch_product_f32(Layout layout, Product p, hipStream_t stream);
+// shares of the reduction that a product of one split per tile would leave the GPU idle without
+int32_t product_splits(int dtype, int64_t M, int64_t N, int64_t K);
+// out[j] = sum over i < count of part[i*n + j], in a fixed order; out fp32 or bf16
+hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* out, int dtype, hipStream_t stream);
+// the same for 2 n columns, the first n to out and the others to out2 (either may be nullptr)
+hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* out, float* out2, hipStream_t stream);
+
+// dZ = G act'(Z) (dZ nullptr: act is none and dZ is G) and, with part, the partial column
+// sums of dZ over act_grad_shares shares of the rows
+int32_t act_grad_shares(int64_t rows, int64_t N);
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* part, int64_t rows, int32_t N, int act,
+                           int dtype, hipStream_t stream);
+
+// mec_norm.hip
+hipError_t launch_norm(const void* X, int64_t ldx, const float* gamma, const float* beta, void* Y, int64_t ldy, float* mean,
+                       float* rstd, int64_t rows, int32_t C, float eps, int dtype, hipStream_t stream);
+int64_t norm_grad_blocks(int64_t rows);  // each leaves 2 C partial sums
+hipError_t launch_norm_grad(const void* G, int64_t ldg, const void* X, int64_t ldx, const float* gamma, const float* mean,
+                            const float* rstd, void* dX, float* dgamma, float* dbeta, float* part, int64_t rows, int32_t C,
+                            int dtype, hipStream_t stream);
+
+// mec_orth.hip
+int64_t orth_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int dtype);
+hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, int64_t rows, int64_t cols, int32_t steps,
+                       float a, float b, float c, float eps, int dtype, hipStream_t stream);
+
+}  // namespace mec
+
+#if defined(__HIP__)
+#include "mec_mfma.h"
+
+namespace mec {
+
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+
+// e^x and 1/x: within an ulp or two of the type for fp32 outputs; for bf16 outputs (FAST) the
+// hardware's exp2 and reciprocal, whose 2^-22 or so (e^x: 2^-24 |x|) the rounding covers
+template <bool FAST>
+__device__ inline float exp_of(float x) { return FAST ? __expf(x) : expf(x); }
+template <bool FAST>
+__device__ inline float reciprocal(float x) { return FAST ? __builtin_amdgcn_rcpf(x) : 1.0f / x; }
+
+constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;  // sqrt(2/pi)
+
+// act(z), with s(x) = 1 / (1 + e^-x). GELU is the tanh form, z/2 (1 + tanh(c (z + a z^3)))
+// = z s(2 c (z + a z^3)), which keeps its relative accuracy where tanh nears -1. NaN stays
+// NaN in all of them.
+template <bool FAST>
+__device__ inline float act_value(int act, float z) {
+    if (act == kActRelu) return z < 0.0f ? 0.0f : z;
+    if (act == kActNone) return z;
+    const float t = act == kActSilu ? z : 2.0f * kGeluC * (z + kGeluA * z * z * z);
+    return z * reciprocal<FAST>(1.0f + exp_of<FAST>(-t));
+}
+// act'(z) for the two smooth ones. s (1 - s) is taken as e^-|t| s(|t|)^2, without the
+// cancellation of 1 - s; past |z| = 12 GELU's slope is 0 or 1 to fp32 (s (1 - s) < e^-100)
+// where z^3 may overflow.
+template <bool FAST>
+__device__ inline float act_slope(int act, float z) {
+    if (act == kActGelu && fabsf(z) > 12.0f) return z > 0.0f ? 1.0f : 0.0f;
+    const float t = act == kActSilu ? z : 2.0f * kGeluC * (z + kGeluA * z * z * z);
+    const float e = exp_of<FAST>(-fabsf(t)), r = reciprocal<FAST>(1.0f + e);
+    const float s = t < 0.0f ? e * r : r, q = e * r * r;
+    if (act == kActSilu) return q == 0.0f ? s : s + z * q;
+    return s + z * q * (2.0f * kGeluC) * (1.0f + 3.0f * kGeluA * z * z);
+}
+
+__device__ inline float to_float(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+__device__ inline float to_float(float x) { return x; }
+template <class E>
+__device__ inline E from_float(float x);
+template <>
+__device__ inline float from_float<float>(float x) { return x; }
+template <>
+__device__ inline uint16_t from_float<uint16_t>(float x) {  // to nearest even
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+// 8 consecutive elements of a 16-byte aligned row
+__device__ inline void load8v(const uint16_t* src, float* v) {
+    const u32x4v w = *reinterpret_cast<const u32x4v*>(src);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+        v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+    }
+}
+__device__ inline void load8v(const float* src, float* v) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4v w = *reinterpret_cast<const f32x4v*>(src + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = w[e];
+    }
+}
+__device__ inline void store8v(uint16_t* dst, const float* v) {
+    u32x4v w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        w[e] = (uint32_t)from_float<uint16_t>(v[2 * e]) | (uint32_t)from_float<uint16_t>(v[2 * e + 1]) << 16;
+    *reinterpret_cast<u32x4v*>(dst) = w;
+}
+__device__ inline void store8v(float* dst, const float* v) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4v*>(dst + 4 * h) = f32x4v{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+}
+
+// 8 outputs (m, n .. n + 7) from their sums v
+template <class E>
+__device__ inline void finish8(const Product& p, int64_t m, int32_t n, int32_t bat, int32_t split, float* v) {
+    if (p.splits > 1) {
+        float* const to = p.part + ((int64_t)split * p.M + m) * p.N + n;
+        if (p.vec) {
+            store8v(to, v);
+        } else {
+            for (int e = 0; e < 8 && n + e < p.N; ++e) to[e] = v[e];
+        }
+        return;
+    }
+    const int cnt = p.N - n < 8 ? p.N - n : 8;
+    float r[8] = {};
+    if (p.R) {
+        const E* const from = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;
+        if (p.vec) {
+            load8v(from, r);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = e < cnt ? to_float(from[e]) : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] *= p.alpha;
+        if (p.bias) v[e] += p.bias[n + (e < cnt ? e : cnt - 1)];
+        if (p.R && p.res_first) v[e] += p.beta * r[e];
+    }
+    if (p.Z) {
+        E* const to = static_cast<E*>(p.Z) + m * p.ldz + n;
+        if (p.vec) {
+            store8v(to, v);
+        } else {
+            for (int e = 0; e < cnt; ++e) to[e] = from_float<E>(v[e]);
+        }
+    }
+    constexpr bool FAST = sizeof(E) == 2;
+    if (p.act == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActRelu, v[e]);
+    } else if (p.act == kActSilu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActSilu, v[e]);
+    } else if (p.act == kActGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActGelu, v[e]);
+    }
+    if (p.R && !p.res_first) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += p.beta * r[e];
+    }
+    E* const to = static_cast<E*>(p.Y) + bat * p.y_batch + m * p.ldy + n;
+    if (p.vec) {
+        store8v(to, v);
+    } else {
+        for (int e = 0; e < cnt; ++e) to[e] = from_float<E>(v[e]);
+    }
+}
+
+// A wave's BM x BN blocks of 32 x 32 sums, as the products leave them with B's columns as
+// the instruction's rows (lane l holds m = l % 32 and, in register v, n = acc_row(v, l)),
+// through `mine`, 32 rows of 32*BN + 4 floats of LDS that only this wave uses: rows are
+// read back whole, so that Y, Z and R move in runs of 64*BN (bf16) or 128*BN bytes.
+template <class E, int BM, int BN>
+__device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN], float* mine, int32_t m0, int32_t n0,
+                                int32_t bat, int32_t split, int lane) {
+    constexpr int PITCH = 32 * BN + 4, LPR = 4 * BN, RPP = 64 / LPR;
+#pragma unroll
+    for (int i = 0; i < BM; ++i) {
+        asm volatile("" ::: "memory");  // the wave's LDS accesses stay in this order
+#pragma unroll
+        for (int j = 0; j < BN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4v*>(mine + (lane & 31) * PITCH + j * 32 + q * 8 + (lane >> 5) * 4) =
+                    f32x4v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int s = 0; s < 32 / RPP; ++s) {
+            const int row = s * RPP + lane / LPR, col = (lane % LPR) * 8;
+            float v[8];
+            load8v(mine + row * PITCH + col, v);
+            const int32_t m = m0 + i * 32 + row, n = n0 + col;
+            if (m < p.M && n < p.N) finish8<E>(p, m, n, bat, split, v);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Tile t of a grid of m_tiles x n_tiles: runs of `group` rows of tiles, column by column,
+// so that the workgroups in flight share rows of A and columns of B in their XCD's L2.
+__device__ inline void tile_of(uint32_t t, uint32_t m_tiles, uint32_t n_tiles, uint32_t group, uint32_t& mt, uint32_t& nt) {
+    const uint32_t per = group * n_tiles, g = t / per, first = g * group;
+    const uint32_t rows = m_tiles - first < group ? m_tiles - first : group;
+    const uint32_t r = t - g * per;
+    nt = r / rows;
+    mt = first + r - nt * rows;
+}
+
+}  // namespace mec
+#endif
