@@ -341,12 +341,8 @@ int first_error(std::initializer_list<int> codes) {
 
 bool valid_act(int act) { return act >= MEC_ACT_NONE && act <= MEC_ACT_GELU; }
 
-hipError_t launch_product(mec::Layout layout, const mec::Product& p, int dtype, hipStream_t st) {
-    return dtype == MEC_F32 ? mec::launch_product_f32(layout, p, st) : mec::launch_product_bf16(layout, p, st);
-}
-
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
-    const int64_t s = mec::product_splits(dtype, i_c, k_c, rows);
+    const int64_t s = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, true).splits;
     const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = mec::act_grad_shares(rows, k_c) * k_c * 4;
     return dk > db ? dk : db;
 }
@@ -382,7 +378,7 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     p.alpha = p.beta = 1.0f;
     p.splits = p.batch = 1;
     clear_stale_error();
-    return hip_status(launch_product(mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
+    return hip_status(mec::launch_product(mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
 }
 
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
@@ -432,7 +428,7 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
         p.M = (int32_t)rows;
         p.N = i_c;
         p.K = k_c;
-        rc = hip_status(launch_product(mec::Layout::kXKt, p, dtype, st), "gradient of the input");
+        rc = hip_status(mec::launch_product(mec::Layout::kXKt, p, dtype, st), "gradient of the input");
         if (rc != MEC_OK) return rc;
     }
     if (dK) {
@@ -445,11 +441,11 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
         p.M = i_c;
         p.N = k_c;
         p.K = (int32_t)rows;
-        p.splits = mec::product_splits(dtype, i_c, k_c, rows);
         p.part = part;
-        rc = hip_status(launch_product(mec::Layout::kXtK, p, dtype, st), "gradient of the kernel");
-        if (rc == MEC_OK && p.splits > 1)
-            rc = hip_status(mec::launch_sum_parts(part, p.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
+        const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, true);
+        rc = hip_status(mec::launch_product(plan, mec::Layout::kXtK, p, dtype, st), "gradient of the kernel");
+        if (rc == MEC_OK && plan.splits > 1)
+            rc = hip_status(mec::launch_sum_parts(part, plan.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
     }
     return rc;
 }
@@ -583,6 +579,38 @@ int mec_internal_wgrad(int kernel, const void* A, const float* G, float* dK, voi
     return hip_status(mec::launch_wgrad_by((mec::WgradKernel)kernel, s, static_cast<const float*>(A), G,
                                            static_cast<float*>(workspace), dK, (hipStream_t)stream, fused),
                       "one kernel's wgrad products");
+}
+
+int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
+    const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split != 0);
+    return p.kernel + 16 * p.splits;
+}
+
+int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits, int M, int N,
+                         int K, int64_t lda, int64_t ldb, int64_t ldy, int dtype, void* stream) {
+    if (layout < 0 || layout > 2 || !valid_dtype(dtype) || !A || !B || !Y || M < 1 || N < 1 || K < 1 || splits < 1 ||
+        (splits > 1 && !part))
+        return MEC_ERR_INVALID_ARG;
+    mec::Product p{};
+    p.A = A;
+    p.B = B;
+    p.Y = Y;
+    p.part = part;
+    p.lda = lda;
+    p.ldb = ldb;
+    p.ldy = ldy;
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    p.alpha = 1.0f;
+    p.batch = 1;
+    clear_stale_error();
+    const hipError_t e = mec::launch_product({kernel, splits}, (mec::Layout)layout, p, dtype, (hipStream_t)stream);
+    if (e == hipErrorNotSupported) return MEC_ERR_UNSUPPORTED;
+    int rc = hip_status(e, "one kernel's product");
+    if (rc == MEC_OK && splits > 1)
+        rc = hip_status(mec::launch_sum_parts(part, splits, (int64_t)M * N, Y, dtype, (hipStream_t)stream), "sum");
+    return rc;
 }
 
 int mec_internal_wgrad_route(int i_n, int i_h, int i_w, int i_c, int k_h, int k_w, int k_c, int s_h, int s_w) {

@@ -234,6 +234,12 @@ extern "C" int mec_internal_wgrad(int kernel, const void* A, const float* G, flo
                                   int s_h, int s_w, int fused, void* stream);
 extern "C" int mec_internal_dgrad_gemm(int tile, const float* G, const float* K, float* dL, int i_n, int i_h, int i_w,
                                        int i_c, int k_h, int k_w, int k_c, int s_h, int s_w, void* stream);
+// The kernel that a product of the layer operators takes, plus 16 times its shares.
+extern "C" int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split);
+// A plain product of the layer operators (mec_product.h) by one kernel: 0 the small one, from
+// 1 the tile kernels; Y's rows are dense where splits > 1 (part: splits x M x N floats).
+extern "C" int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits,
+                                    int M, int N, int K, int64_t lda, int64_t ldb, int64_t ldy, int dtype, void* stream);
 
 #if defined(__HIP__)
 namespace mec {

@@ -33,10 +33,6 @@ struct Cfg {
     static_assert(TM * 8 % THREADS == 0 && TN * 8 % THREADS == 0 && LDS <= 160 * 1024, "tile");
 };
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) char lds_char;
-
 __device__ inline uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 __device__ inline const char* scalar(const char* x) {
     const uint64_t v = (uint64_t)x;
@@ -59,22 +55,6 @@ __device__ inline void to_lds16(u32x4v rsrc, uint32_t voff, uint32_t lds) {
         : "=&s"(saved)
         : "s"(lds), "v"(voff), "s"(rsrc)
         : "memory");
-}
-
-// 16 bytes at any 2-byte boundary
-__device__ inline u32x4v load_any(const uint16_t* src) {
-    struct __attribute__((packed, aligned(2))) Any {
-        u32x4v v;
-    };
-    return reinterpret_cast<const Any*>(src)->v;
-}
-__device__ inline u32x4v load_some(const uint16_t* src, int64_t have) {  // its first `have` elements, then zeros
-    if (have >= 8) return load_any(src);
-    u32x4v w = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < have) w[e / 2] |= (uint32_t)src[e] << (16 * (e % 2));
-    return w;
 }
 
 // One operand's T rows (stored along the reduction) or columns (TR: across it) of a tile.
@@ -167,10 +147,9 @@ struct Operand {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int k = kk * 16 + 8 * (lane >> 5) + 4 * s + (p >> 2);
-                const char* const at = from + k * (T * 2) + ((c16 ^ (k & SW)) << 5) + (p & 3) * 8;
-                h[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)at);
+                h[s] = read_tr(from + k * (T * 2) + ((c16 ^ (k & SW)) << 5) + (p & 3) * 8);
             }
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            return join_tr(h[0], h[1]);
         } else {
             const int r = blk * 32 + (lane & 31), g = 2 * kk + (lane >> 5);
             return *reinterpret_cast<const bf16x8*>(from + r * 128 + ((g ^ (r & 7)) << 4));
@@ -282,35 +261,29 @@ hipError_t run(Product p, hipStream_t stream) {
 }
 
 template <Layout L>
-hipError_t pick(const Product& p, hipStream_t stream) {
-    return run<2, 2, 2, 2, L>(p, stream);
+hipError_t pick(const Product& p, int tile, hipStream_t stream) {
+    switch (tile) {
+        case 1: return run<2, 2, 2, 2, L>(p, stream);
+        case 2: return run<4, 2, 2, 4, L>(p, stream);
+        case 3: return run<1, 2, 2, 2, L>(p, stream);
+        case 4: return run<1, 1, 2, 2, L>(p, stream);
+        default: return hipErrorNotSupported;
+    }
 }
 
 }  // namespace
 
-hipError_t launch_product_bf16(Layout layout, Product p, hipStream_t stream) {
+hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream) {
     auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 8 == 0); };
     p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0;
     // the dimension that each operand's rows run along has to be whole granules
     const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
     p.clean = rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;
     switch (layout) {
-        case Layout::kXK: return pick<Layout::kXK>(p, stream);
-        case Layout::kXKt: return pick<Layout::kXKt>(p, stream);
-        default: return pick<Layout::kXtK>(p, stream);
+        case Layout::kXK: return pick<Layout::kXK>(p, tile, stream);
+        case Layout::kXKt: return pick<Layout::kXKt>(p, tile, stream);
+        default: return pick<Layout::kXtK>(p, tile, stream);
     }
-}
-
-// Shares of the reduction: as many as fill 512 workgroups of the products' 128-wide tiles,
-// with at least 512 elements of the reduction each and none empty.
-int32_t product_splits(int, int64_t M, int64_t N, int64_t K) {
-    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), chunks = (K + kKT - 1) / kKT;
-    int64_t s = 512 / tiles;
-    if (s > chunks / 8) s = chunks / 8;
-    if (s > 64) s = 64;
-    if (s < 2) return 1;
-    const int64_t per = (chunks + s - 1) / s;
-    return (int32_t)((chunks + per - 1) / per);
 }
 
 }  // namespace mec

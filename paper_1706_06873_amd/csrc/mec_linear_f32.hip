@@ -22,7 +22,7 @@ struct Cfg {
     static constexpr int APL = TM * kKT * 2, BPL = TN * kKT * 2, STAGE = 3 * (APL + BPL);  // bytes (of a plane)
     static constexpr int EPI = WAVES * 32 * (32 * BN + 4) * 4;
     static constexpr int LDS = 2 * STAGE > EPI ? 2 * STAGE : EPI;
-    static constexpr int kPerSimd = WAVES == 8 ? 2 : (LDS <= 80 * 1024 ? 2 : 1);
+    static constexpr int kPerSimd = WAVES == 8 ? 2 : (LDS <= 53 * 1024 ? 3 : LDS <= 80 * 1024 ? 2 : 1);
     static_assert(TM * kG % THREADS == 0 && TN * kG % THREADS == 0 && THREADS % TM == 0 && THREADS % TN == 0 && LDS <= 158 * 1024, "tile");
 };
 
@@ -185,8 +185,8 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
         MEC_MM(0, 2, low)
 #undef MEC_MM
     };
-    // one chunk at a time in registers: it is requested while the first half of the chunk
-    // before the last is multiplied, and split into the other stage a chunk later
+    // One chunk at a time in registers: it is requested under the second half of the chunk
+    // before the last and split into the other stage under the first half of the last.
     Frags f;
     Regs r;
     load(r);
@@ -263,20 +263,25 @@ hipError_t run(Product p, hipStream_t stream) {
 }
 
 template <Layout L>
-hipError_t pick(const Product& p, hipStream_t stream) {
-    return run<1, 2, 4, 1, L>(p, stream);
+hipError_t pick(const Product& p, int tile, hipStream_t stream) {
+    switch (tile) {
+        case 1: return run<1, 2, 4, 1, L>(p, stream);
+        case 2: return run<2, 2, 4, 2, L>(p, stream);
+        case 3: return run<1, 1, 2, 2, L>(p, stream);
+        default: return hipErrorNotSupported;
+    }
 }
 
 }  // namespace
 
-hipError_t launch_product_f32(Layout layout, Product p, hipStream_t stream) {
+hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream) {
     auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 4 == 0); };
     p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0 &&
             p.y_batch % 4 == 0 && p.r_batch % 4 == 0;
     switch (layout) {
-        case Layout::kXK: return pick<Layout::kXK>(p, stream);
-        case Layout::kXKt: return pick<Layout::kXKt>(p, stream);
-        default: return pick<Layout::kXtK>(p, stream);
+        case Layout::kXK: return pick<Layout::kXK>(p, tile, stream);
+        case Layout::kXKt: return pick<Layout::kXKt>(p, tile, stream);
+        default: return pick<Layout::kXtK>(p, tile, stream);
     }
 }
 

@@ -1,0 +1,280 @@
+// Matrix products of the layer operators with few outputs, where the tile kernels would
+// leave the GPU to a few workgroups that take one chunk after another: a workgroup computes
+// 32 x 32 outputs, its 16 waves share the reduction (each takes one run of it, with loads of
+// its own and no barriers) and their sums are joined in LDS in the order of the waves. Bound
+// by the latency of a few rounds of loads.
+//
+// fp32: operands go from memory to registers, are split there and multiplied (mec_split.h).
+// bf16: operands stored along the reduction likewise (a fragment is 16 bytes of a row); those
+// stored across it pass through a patch of LDS of the wave's own, for the transposing reads.
+#include "mec_product.h"
+#include "mec_split.h"
+
+namespace mec {
+namespace {
+
+constexpr int kWaves = 16, kPitch = 36;  // floats of a row of a wave's sums in LDS
+
+struct Slice {
+    int32_t k0, k1;  // this wave's run of the reduction
+};
+
+// The sums of the waves, joined: thread t finishes output (t / 32, t % 32).
+template <class E>
+__device__ inline void join(const Product& p, const floatx16& acc, float* sums, int32_t m0, int32_t n0, int32_t bat, int waves,
+                            int wave, int lane) {
+    if (wave < waves) {
+        float* const mine = sums + wave * 32 * kPitch + (lane & 31) * kPitch + (lane >> 5) * 4;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4v*>(mine + q * 8) = f32x4v{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    }
+    __syncthreads();
+    const int m = (int)threadIdx.x / 32, n = (int)threadIdx.x % 32;
+    if (m0 + m >= p.M || n0 + n >= p.N) return;
+    float v[1] = {0.0f};
+    for (int w = 0; w < waves; ++w) v[0] += sums[w * 32 * kPitch + m * kPitch + n];
+    finish<E, 1>(p, m0 + m, n0 + n, bat, 0, v);
+}
+
+struct Place {
+    int32_t m0, n0, bat, waves;
+    Slice k;
+};
+__device__ inline Place place(const Product& p, int wave) {
+    Place t;
+    const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    t.bat = (int32_t)(b / tiles);
+    const uint32_t r = b - (uint32_t)t.bat * tiles, mt = r / (uint32_t)p.n_tiles;
+    t.m0 = (int32_t)mt * 32;
+    t.n0 = (int32_t)(r - mt * (uint32_t)p.n_tiles) * 32;
+    const int32_t run = p.chunks * 16;  // of the reduction, a wave
+    t.waves = (p.K + run - 1) / run;
+    t.k.k0 = wave * run;
+    t.k.k1 = t.k.k0 + run < p.K ? t.k.k0 + run : p.K;
+    return t;
+}
+
+// ---------------------------------------------------------------- fp32
+// 8 k of row (column) r: stored along (stride 1) or across (stride ld) the reduction
+template <bool TR>
+__device__ inline void fetch(const float* base, int64_t ld, int32_t k, int32_t k1, float* x) {
+    if constexpr (TR) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int32_t at = k + e < k1 ? k + e : k1 - 1;
+            const float v = base[at * ld];
+            x[e] = k + e < k1 ? v : 0.0f;
+        }
+    } else if (k + 8 <= k1) {
+        struct __attribute__((packed, aligned(4))) Any {
+            f32x4v v;
+        };
+        const f32x4v a = reinterpret_cast<const Any*>(base + k)->v, b = reinterpret_cast<const Any*>(base + k + 4)->v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = a[e];
+            x[4 + e] = b[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e < k1 ? base[k + e] : 0.0f;
+    }
+}
+
+template <Layout L>
+__global__ __launch_bounds__(64 * kWaves) void small_f32_kernel(Product p) {
+    constexpr bool AT = L == Layout::kXtK, BT = L != Layout::kXKt;
+    constexpr int U = 2;  // steps of 16 k in flight
+    __shared__ __align__(16) float sums[kWaves * 32 * kPitch];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place t = place(p, wave);
+    floatx16 acc = {};
+    if (wave < t.waves) {
+        // rows and columns past the last are copies of it
+        const int32_t m = t.m0 + (lane & 31) < p.M ? t.m0 + (lane & 31) : p.M - 1;
+        const int32_t n = t.n0 + (lane & 31) < p.N ? t.n0 + (lane & 31) : p.N - 1;
+        const float* const a = static_cast<const float*>(p.A) + t.bat * p.a_batch + (AT ? (int64_t)m : m * p.lda);
+        const float* const b = static_cast<const float*>(p.B) + t.bat * p.b_batch + (BT ? (int64_t)n : n * p.ldb);
+        floatx16 low = {};
+        uint32_t lost = 0;
+        for (int32_t k = t.k.k0; k < t.k.k1; k += 16 * U) {
+            float x[U][8], y[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                fetch<AT>(a, p.lda, k + 16 * u + 8 * (lane >> 5), t.k.k1, x[u]);
+                fetch<BT>(b, p.ldb, k + 16 * u + 8 * (lane >> 5), t.k.k1, y[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                u32x4 xs[3], ys[3];
+                split8(x[u], xs[0], xs[1], xs[2], lost);
+                split8(y[u], ys[0], ys[1], ys[2], lost);
+                auto mm = [&](int i, int j, floatx16& to) {
+                    to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ys[j]), __builtin_bit_cast(bf16x8, xs[i]),
+                                                                 to, 0, 0, 0);
+                };
+                mm(0, 0, acc);
+                mm(1, 0, low);
+                mm(0, 1, low);
+                mm(1, 1, low);
+                mm(2, 0, low);
+                mm(0, 2, low);
+            }
+        }
+        uint32_t most = 0;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            acc[v] += low[v];
+            const float x = acc[v];
+            const uint32_t bits = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+            most = bits > most ? bits : most;
+        }
+        if (__any((lost & 0xffffu) != 0) || __any(most >= 0x7f800000u)) {  // values the split does not hold
+            floatx16 sum = {};
+            plain_products(
+                sum, (uint32_t)(t.k.k1 - t.k.k0 + 15) / 16u,
+                [&](uint32_t s, float* x) { fetch<BT>(b, p.ldb, t.k.k0 + (int32_t)s * 16 + 8 * (lane >> 5), t.k.k1, x); },
+                [&](uint32_t s, float* x) { fetch<AT>(a, p.lda, t.k.k0 + (int32_t)s * 16 + 8 * (lane >> 5), t.k.k1, x); });
+            acc = sum;
+        }
+    }
+    join<float>(p, acc, sums, t.m0, t.n0, t.bat, t.waves, wave, lane);
+}
+
+// ---------------------------------------------------------------- bf16
+constexpr int kRun = 64;                  // k per turn: 4 fragments of each operand
+constexpr int kPatch = kRun * 32 * 2;     // bytes of a wave's patch: 64 rows of 32 columns
+
+// The 4 fragments of an operand for the 64 k from k on, in two parts: loads, and what makes
+// fragments of them. CLEAN: 16-byte rows of whole granules.
+template <bool TR, bool CLEAN>
+struct Turn {
+    u32x4v w[4];
+    // base: the tile's first row (column); r: rows (columns) there are from it on
+    __device__ inline void load(const uint16_t* base, int64_t ld, int32_t r, int32_t k, int32_t k1, int lane) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TR) {  // row k + 16 i + lane / 4, granule lane % 4 of its 32 columns
+                const int32_t at = k + 16 * i + (lane >> 2), c = (lane & 3) * 8;
+                const uint16_t* const src = base + (at < k1 ? at : k1 - 1) * ld;
+                if constexpr (CLEAN) {
+                    w[i] = *reinterpret_cast<const u32x4v*>(src + (c < r ? c : r - 8));
+                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
+                } else {
+                    w[i] = load_some(src + c, at < k1 ? r - c : 0);
+                }
+            } else {
+                const int32_t at = k + 16 * i + 8 * (lane >> 5);
+                const uint16_t* const src = base + ((lane & 31) < r ? (lane & 31) : r - 1) * ld;
+                if constexpr (CLEAN) {
+                    w[i] = *reinterpret_cast<const u32x4v*>(src + (at < k1 ? at : k1 - 8));
+                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
+                } else {
+                    w[i] = load_some(src + at, k1 - at);
+                }
+            }
+        }
+    }
+    // rows of the patch are 64 bytes; their two 16-column blocks change places every second
+    // pair of rows, so that the 4 rows that 16 lanes read lie on different banks
+    __device__ inline void put(char* patch, int lane) const {
+        if constexpr (TR)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * i + (lane >> 2), c = lane & 3;
+                *reinterpret_cast<u32x4v*>(patch + row * 64 + ((c ^ (row & 2)) << 4)) = w[i];
+            }
+    }
+    __device__ inline bf16x8 frag(const char* patch, int i, int lane) const {
+        if constexpr (!TR) return __builtin_bit_cast(bf16x8, w[i]);
+        const int q = lane & 15, block = (lane >> 4) & 1;
+        s16x4 h[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int row = 16 * i + 8 * (lane >> 5) + 4 * s + (q >> 2);
+            h[s] = read_tr(patch + row * 64 + (((block << 1) ^ (row & 2)) << 4) + (q & 3) * 8);
+        }
+        return join_tr(h[0], h[1]);
+    }
+};
+
+template <Layout L, bool CLEAN>
+__global__ __launch_bounds__(64 * kWaves) void small_bf16_kernel(Product p) {
+    constexpr bool AT = L == Layout::kXtK, BT = L != Layout::kXKt;
+    constexpr int PATCHES = (AT ? kPatch : 0) + (BT ? kPatch : 0);
+    constexpr int SUMS = kWaves * 32 * kPitch * 4;
+    __shared__ __align__(16) char lds[kWaves * PATCHES > SUMS ? kWaves * PATCHES : SUMS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place t = place(p, wave);
+    floatx16 acc = {};
+    if (wave < t.waves) {
+        const uint16_t* const a = static_cast<const uint16_t*>(p.A) + t.bat * p.a_batch + (AT ? (int64_t)t.m0 : t.m0 * p.lda);
+        const uint16_t* const b = static_cast<const uint16_t*>(p.B) + t.bat * p.b_batch + (BT ? (int64_t)t.n0 : t.n0 * p.ldb);
+        char* const patch_b = lds + wave * PATCHES;
+        char* const patch_a = patch_b + (BT ? kPatch : 0);
+        Turn<AT, CLEAN> ta;
+        Turn<BT, CLEAN> tb;
+        ta.load(a, p.lda, p.M - t.m0, t.k.k0, t.k.k1, lane);
+        tb.load(b, p.ldb, p.N - t.n0, t.k.k0, t.k.k1, lane);
+        for (int32_t k = t.k.k0; k < t.k.k1; k += kRun) {
+            bf16x8 fa[4], fb[4];
+            ta.put(patch_a, lane);
+            tb.put(patch_b, lane);
+            if constexpr (AT || BT) {  // the wave's LDS accesses stay in this order
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fa[i] = ta.frag(patch_a, i, lane);
+                fb[i] = tb.frag(patch_b, i, lane);
+            }
+            if (k + kRun < t.k.k1) {
+                ta.load(a, p.lda, p.M - t.m0, k + kRun, t.k.k1, lane);
+                tb.load(b, p.ldb, p.N - t.n0, k + kRun, t.k.k1, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i], fa[i], acc, 0, 0, 0);
+            if constexpr (AT || BT) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    }
+    __syncthreads();
+    join<uint16_t>(p, acc, reinterpret_cast<float*>(lds), t.m0, t.n0, t.bat, t.waves, wave, lane);
+}
+
+template <Layout L>
+hipError_t run(const Product& p, int dtype, hipStream_t stream) {
+    const dim3 grid((uint32_t)((int64_t)p.m_tiles * p.n_tiles * p.batch)), block(64 * kWaves);
+    if (!dtype) hipLaunchKernelGGL(small_f32_kernel<L>, grid, block, 0, stream, p);
+    else if (p.clean) hipLaunchKernelGGL((small_bf16_kernel<L, true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((small_bf16_kernel<L, false>), grid, block, 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream) {
+    p.m_tiles = (p.M + 31) / 32;
+    p.n_tiles = (p.N + 31) / 32;
+    if ((int64_t)p.m_tiles * p.n_tiles * p.batch > 0x3fffff || p.splits > 1) return hipErrorInvalidValue;
+    // a wave's run: whole steps of 16 k
+    const int64_t steps = ((int64_t)p.K + 15) / 16;
+    p.chunks = (int32_t)((steps + kWaves - 1) / kWaves);
+    if (dtype) {
+        const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
+        p.clean = !(((uintptr_t)p.A | (uintptr_t)p.B) & 15u) && p.lda % 8 == 0 && p.ldb % 8 == 0 && a_run % 8 == 0 &&
+                  b_run % 8 == 0 && p.a_batch % 8 == 0 && p.b_batch % 8 == 0;
+    }
+    switch (layout) {
+        case Layout::kXK: return run<Layout::kXK>(p, dtype, stream);
+        case Layout::kXKt: return run<Layout::kXKt>(p, dtype, stream);
+        default: return run<Layout::kXtK>(p, dtype, stream);
+    }
+}
+
+}  // namespace mec

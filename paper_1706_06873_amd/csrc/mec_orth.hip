@@ -111,7 +111,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.K = (int32_t)(n / m);
         p.a_batch = p.b_batch = n;
         p.y_batch = p.r_batch = m * m;
-        e = launch_product_f32(rows <= cols ? Layout::kXKt : Layout::kXtK, p, stream);
+        e = launch_product(rows <= cols ? Layout::kXKt : Layout::kXtK, p, 0, stream);
         if (e != hipSuccess) break;
         // P = c A^2 + b A (A is symmetric: A A^T)
         p.A = p.B = A;
@@ -122,7 +122,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.a_batch = p.b_batch = m * m;
         p.alpha = c;
         p.beta = b;
-        e = launch_product_f32(Layout::kXKt, p, stream);
+        e = launch_product(Layout::kXKt, p, 0, stream);
         if (e != hipSuccess) break;
         // X
         p.alpha = 1.0f;
@@ -140,7 +140,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
             p.B = from;
             p.ldb = cols;
             p.b_batch = n;
-            e = launch_product_f32(Layout::kXK, p, stream);
+            e = launch_product(Layout::kXK, p, 0, stream);
         } else {
             p.A = from;
             p.lda = cols;
@@ -148,7 +148,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
             p.B = P;
             p.ldb = m;
             p.b_batch = m * m;
-            e = launch_product_f32(Layout::kXKt, p, stream);
+            e = launch_product(Layout::kXKt, p, 0, stream);
         }
     }
     if (e == hipSuccess && dtype) {

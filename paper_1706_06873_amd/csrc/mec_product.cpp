@@ -1,0 +1,71 @@
+// Which kernel computes a product of the layer operators. The times of each are modelled and
+// the least taken: a tile kernel's busiest compute unit takes ceil(tiles / 256) tiles, as many
+// at a time as fit, at the cost below per chunk of the reduction with 1, 2, .. resident and
+// per tile for its start and end; the small kernel's one workgroup at a time, at a cost per
+// round and per element of the reduction. All in us, measured on this GPU on long and short
+// reductions over few and many tiles (M x N x K, us): bf16 16384 x 4096 x 4096 256x256 471,
+// 128x128 526, 64x128 619, 64x64 746; 1024 x 1024 x 1024 34, 16.0, 11.5, 8.5 and small 19;
+// 512 x 512 x 64 small 4.0, 128x128 7.4. fp32 16384 x 4096 x 1024 256x128 694, 128x64 862,
+// 64x64 928; 1024 x 1024 x 1024 69, 37, 26 and small 36; 512 x 512 x 512 small 6.7.
+#include "mec_product.h"
+
+namespace mec {
+namespace {
+
+struct TileCost {
+    int tm, tn, fit;
+    double chunk[5], ends;
+};
+// by the kernels' numbers, from 1
+constexpr TileCost kBf16[] = {{128, 128, 2, {0.60, 0.93}, 6.0},
+                              {256, 256, 1, {1.55}, 12.0},
+                              {64, 128, 3, {0.42, 0.65, 0.80}, 4.8},
+                              {64, 64, 5, {0.30, 0.47, 0.62, 0.78, 0.87}, 3.7}};
+constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 7.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
+    const int64_t busiest = ceil_div(tiles, 256), rounds = busiest / t.fit, rest = busiest % t.fit;
+    double us = (double)rounds * ((double)chunks * t.chunk[t.fit - 1] + t.ends);
+    if (rest) us += (double)chunks * t.chunk[rest - 1] + t.ends;
+    return us;
+}
+
+}  // namespace
+
+ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split) {
+    const int64_t small_rounds = ceil_div(ceil_div(M, 32) * ceil_div(N, 32) * batch, 256);
+    ProductPlan best{0, 1};
+    double best_us = (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K);
+    const TileCost* const tiles = dtype ? kBf16 : kF32;
+    const int count = dtype ? 4 : 3;
+    const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
+    for (int i = 0; i < count; ++i) {
+        const int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn) * batch;
+        for (int64_t s = 1; s <= 64; s = s < 4 ? s + 1 : s + s / 4) {
+            // shares of at least 4 chunks of 64, none empty, and partial sums of at most 256 MB
+            if (s > 1 && (!may_split || batch > 1 || shares < 4 * s || s * M * N > (int64_t(1) << 26))) break;
+            const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
+            double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
+            if (real > 1) us += 3.0 + (double)(real * M * N) / 8e5;  // the sum of the shares
+            if (us < best_us) {
+                best = {i + 1, (int32_t)real};
+                best_us = us;
+            }
+        }
+    }
+    return best;
+}
+
+hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {
+    p.splits = plan.splits;
+    if (plan.kernel == 0) return p.splits > 1 ? hipErrorNotSupported : launch_product_small(layout, p, dtype, stream);
+    return dtype ? launch_product_bf16(layout, p, plan.kernel, stream) : launch_product_f32(layout, p, plan.kernel, stream);
+}
+
+hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream) {
+    return launch_product(plan_product(layout, dtype, p.M, p.N, p.K, p.batch, false), layout, p, dtype, stream);
+}
+
+}  // namespace mec

@@ -42,11 +42,22 @@ struct Product {
     int32_t clean;                     // 16-byte rows of A and B
 };
 
-// Enqueue the product; A, B, Z, R, Y bf16 or fp32. splits > 1 leaves the partial sums.
-hipError_t launch_product_bf16(Layout layout, Product p, hipStream_t stream);
-hipError_t launch_product_f32(Layout layout, Product p, hipStream_t stream);
-// shares of the reduction that a product of one split per tile would leave the GPU idle without
-int32_t product_splits(int dtype, int64_t M, int64_t N, int64_t K);
+// Which kernel computes a product, and the shares of its reduction.
+struct ProductPlan {
+    int kernel;  // 0 the small one, from 1 the tiles
+    int32_t splits;
+};
+ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split);
+
+// Enqueue the product (dtype of A, B, Z, R, Y), with p.splits shares that leave their partial
+// sums where it is above 1. hipErrorNotSupported where there is no such kernel.
+hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream);
+hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream);  // mec_linear.hip
+hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream);   // mec_linear_f32.hip
+hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream);  // mec_linear_small.hip
+// by the plan, in one share
+hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream);
+
 // out[j] = sum over i < count of part[i*n + j], in a fixed order; out fp32 or bf16
 hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* out, int dtype, hipStream_t stream);
 // the same for 2 n columns, the first n to out and the others to out2 (either may be nullptr)
@@ -153,64 +164,92 @@ __device__ inline void store8v(float* dst, const float* v) {
     for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4v*>(dst + 4 * h) = f32x4v{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
 }
 
-// 8 outputs (m, n .. n + 7) from their sums v
-template <class E>
-__device__ inline void finish8(const Product& p, int64_t m, int32_t n, int32_t bat, int32_t split, float* v) {
+// 16 bytes at any 2-byte boundary
+__device__ inline u32x4v load_any(const uint16_t* src) {
+    struct __attribute__((packed, aligned(2))) Any {
+        u32x4v v;
+    };
+    return reinterpret_cast<const Any*>(src)->v;
+}
+__device__ inline u32x4v load_some(const uint16_t* src, int64_t have) {  // its first `have` elements, then zeros
+    if (have >= 8) return load_any(src);
+    u32x4v w = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < have) w[e / 2] |= (uint32_t)src[e] << (16 * (e % 2));
+    return w;
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Transposing read of 4 k for each of 16 columns: lane p of 16 gives the address of columns
+// 4*(p % 4) .. + 3 of row k + p / 4, and gets rows k .. k + 3 of column p.
+__device__ inline s16x4 read_tr(const char* at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)at);
+}
+__device__ inline bf16x8 join_tr(s16x4 a, s16x4 b) {
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// V outputs (m, n .. n + V - 1) from their sums v
+template <class E, int V>
+__device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t bat, int32_t split, float* v) {
+    const int cnt = p.N - n < V ? p.N - n : V;
     if (p.splits > 1) {
         float* const to = p.part + ((int64_t)split * p.M + m) * p.N + n;
-        if (p.vec) {
+        if (V == 8 && p.vec) {
             store8v(to, v);
         } else {
-            for (int e = 0; e < 8 && n + e < p.N; ++e) to[e] = v[e];
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < cnt) to[e] = v[e];
         }
         return;
     }
-    const int cnt = p.N - n < 8 ? p.N - n : 8;
-    float r[8] = {};
+    float r[V] = {};
     if (p.R) {
         const E* const from = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;
-        if (p.vec) {
+        if (V == 8 && p.vec) {
             load8v(from, r);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = e < cnt ? to_float(from[e]) : 0.0f;
+            for (int e = 0; e < V; ++e) r[e] = e < cnt ? to_float(from[e]) : 0.0f;
         }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < V; ++e) {
         v[e] *= p.alpha;
         if (p.bias) v[e] += p.bias[n + (e < cnt ? e : cnt - 1)];
         if (p.R && p.res_first) v[e] += p.beta * r[e];
     }
-    if (p.Z) {
-        E* const to = static_cast<E*>(p.Z) + m * p.ldz + n;
-        if (p.vec) {
+    auto store = [&](void* base, int64_t at) {
+        E* const to = static_cast<E*>(base) + at;
+        if (V == 8 && p.vec) {
             store8v(to, v);
         } else {
-            for (int e = 0; e < cnt; ++e) to[e] = from_float<E>(v[e]);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < cnt) to[e] = from_float<E>(v[e]);
         }
-    }
+    };
+    if (p.Z) store(p.Z, m * p.ldz + n);
     constexpr bool FAST = sizeof(E) == 2;
     if (p.act == kActRelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActRelu, v[e]);
+        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActRelu, v[e]);
     } else if (p.act == kActSilu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActSilu, v[e]);
+        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActSilu, v[e]);
     } else if (p.act == kActGelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_value<FAST>(kActGelu, v[e]);
+        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActGelu, v[e]);
     }
     if (p.R && !p.res_first) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += p.beta * r[e];
+        for (int e = 0; e < V; ++e) v[e] += p.beta * r[e];
     }
-    E* const to = static_cast<E*>(p.Y) + bat * p.y_batch + m * p.ldy + n;
-    if (p.vec) {
-        store8v(to, v);
-    } else {
-        for (int e = 0; e < cnt; ++e) to[e] = from_float<E>(v[e]);
-    }
+    store(p.Y, bat * p.y_batch + m * p.ldy + n);
 }
 
 // A wave's BM x BN blocks of 32 x 32 sums, as the products leave them with B's columns as
@@ -238,7 +277,7 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
             float v[8];
             load8v(mine + row * PITCH + col, v);
             const int32_t m = m0 + i * 32 + row, n = n0 + col;
-            if (m < p.M && n < p.N) finish8<E>(p, m, n, bat, split, v);
+            if (m < p.M && n < p.N) finish<E, 8>(p, m, n, bat, split, v);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();

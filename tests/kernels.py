@@ -68,3 +68,30 @@ def dgrad_gemm(tile, G, K, dims):
                                      torch.cuda.current_stream().cuda_stream)
     assert r in (0, UNSUPPORTED), (dims, r)
     return dL if r == 0 else None
+
+
+_i64 = ctypes.c_int64
+_lib.mec_internal_product.argtypes = [_i, _i, _vp, _vp, _vp, _vp] + [_i] * 4 + [_i64] * 3 + [_i, _vp]
+_lib.mec_internal_product_plan.argtypes = [_i] * 7
+XK, XKT, XTK = range(3)                               # Layout
+
+
+def product_plan(layout, dtype, M, N, K, batch=1, may_split=False):
+    """(kernel, shares of the reduction) that a product of the layer operators takes."""
+    r = _lib.mec_internal_product_plan(layout, mec.F32 if dtype == "f32" else mec.BF16, M, N, K, batch, int(may_split))
+    return r % 16, r // 16
+
+
+def product(kernel, layout, A, B, splits=1):
+    """A B by one kernel (0 the small one, from 1 the tiles); A is [m][k] ([k][m] for XTK), B
+    [k][n] ([n][k] for XKT). None where there is no such kernel."""
+    K, M = A.shape if layout == XTK else A.shape[::-1]
+    N = B.shape[0] if layout == XKT else B.shape[1]
+    Y = torch.full((M, N), 7.0, dtype=A.dtype, device=A.device)
+    part = torch.empty(splits * M * N, device=A.device) if splits > 1 else None
+    r = _lib.mec_internal_product(kernel, layout, A.data_ptr(), B.data_ptr(), Y.data_ptr(),
+                                  part.data_ptr() if splits > 1 else None, splits, M, N, K, A.stride(0), B.stride(0), N,
+                                  mec.BF16 if A.dtype == torch.bfloat16 else mec.F32,
+                                  torch.cuda.current_stream().cuda_stream)
+    assert r in (0, UNSUPPORTED), (kernel, layout, A.shape, B.shape, r)
+    return Y if r == 0 else None

@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+import kernels as kn
 import paper_1706_06873_amd as mec
 
 pytestmark = pytest.mark.gpu
@@ -180,6 +181,31 @@ def test_linear_far_values_fp32():
         Y = mec.linear(X.to(DEV), K.to(DEV))
         x, k = X.double(), K.double()
         close(Y, x @ k, 56 * 2.0 ** -23 * (x.abs() @ k.abs()) + 48 * 2.0 ** -126, (scale_x, scale_k))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", [kn.XK, kn.XKT, kn.XTK])
+def test_every_product_kernel(dtype, layout):
+    """Each kernel on shapes that the calls may give to another: tiles with ragged ends, several
+    tiles, one and many chunks, rows with a pitch, and shares of the reduction."""
+    for M, N, K, gap, splits in [(300, 280, 200, 0, 1), (257, 264, 64, 8, 1), (130, 67, 77, 3, 1), (5, 9, 700, 0, 1),
+                                 (264, 520, 1064, 0, 1), (136, 72, 2000, 0, 7), (33, 200, 517, 5, 3)]:
+        g = torch.Generator().manual_seed(M + N + K)
+        a, b = randn(g, M, K).to(dtype), randn(g, K, N).to(dtype)
+        want = a.double() @ b.double()
+        err = (K + 8) * 2.0 ** -23 * (a.double().abs() @ b.double().abs())
+        A = rows_of(a.T.contiguous() if layout == kn.XTK else a, gap)
+        B = rows_of(b.T.contiguous() if layout == kn.XKT else b, gap)
+        ran = 0
+        for kernel in range(8):
+            if splits > 1 and kernel == 0:
+                continue
+            print("[case]", dtype, layout, M, N, K, gap, splits, kernel, flush=True)
+            Y = kn.product(kernel, layout, A, B, splits)
+            if Y is not None:
+                close(Y, want, err + HALF[dtype] * (want.abs() + err), kernel)
+                ran += 1
+        assert ran >= 3
 
 
 def test_linear_in_place_and_shapes():
