@@ -605,7 +605,7 @@ int mec_internal_product(int kernel, int layout, const void* A, const void* B, v
     p.alpha = 1.0f;
     p.batch = 1;
     clear_stale_error();
-    const hipError_t e = mec::launch_product({kernel, splits}, (mec::Layout)layout, p, dtype, (hipStream_t)stream);
+    const hipError_t e = mec::launch_product({kernel, splits, 0.0}, (mec::Layout)layout, p, dtype, (hipStream_t)stream);
     if (e == hipErrorNotSupported) return MEC_ERR_UNSUPPORTED;
     int rc = hip_status(e, "one kernel's product");
     if (rc == MEC_OK && splits > 1)

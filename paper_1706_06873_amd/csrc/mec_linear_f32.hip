@@ -135,8 +135,8 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
     const int64_t k0 = (int64_t)split * p.chunks * kKT;
     const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
     const int chunks = (int)((k1 - k0 + kKT - 1) / kKT);
-    const float* const A = static_cast<const float*>(p.A) + bat * p.a_batch;
-    const float* const B = static_cast<const float*>(p.B) + bat * p.b_batch;
+    const float* const A = a_of<float>(p, bat);
+    const float* const B = b_of<float>(p, bat);
 
     if (tid == 0) lost_s = 0;  // (ordered by the first barriers)
     OpA oa;

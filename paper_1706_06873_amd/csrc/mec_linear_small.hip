@@ -95,8 +95,8 @@ __global__ __launch_bounds__(64 * kWaves) void small_f32_kernel(Product p) {
         // rows and columns past the last are copies of it
         const int32_t m = t.m0 + (lane & 31) < p.M ? t.m0 + (lane & 31) : p.M - 1;
         const int32_t n = t.n0 + (lane & 31) < p.N ? t.n0 + (lane & 31) : p.N - 1;
-        const float* const a = static_cast<const float*>(p.A) + t.bat * p.a_batch + (AT ? (int64_t)m : m * p.lda);
-        const float* const b = static_cast<const float*>(p.B) + t.bat * p.b_batch + (BT ? (int64_t)n : n * p.ldb);
+        const float* const a = a_of<float>(p, t.bat) + (AT ? (int64_t)m : m * p.lda);
+        const float* const b = b_of<float>(p, t.bat) + (BT ? (int64_t)n : n * p.ldb);
         floatx16 low = {};
         uint32_t lost = 0;
         for (int32_t k = t.k.k0; k < t.k.k1; k += 16 * U) {
@@ -210,8 +210,8 @@ __global__ __launch_bounds__(64 * kWaves) void small_bf16_kernel(Product p) {
     const Place t = place(p, wave);
     floatx16 acc = {};
     if (wave < t.waves) {
-        const uint16_t* const a = static_cast<const uint16_t*>(p.A) + t.bat * p.a_batch + (AT ? (int64_t)t.m0 : t.m0 * p.lda);
-        const uint16_t* const b = static_cast<const uint16_t*>(p.B) + t.bat * p.b_batch + (BT ? (int64_t)t.n0 : t.n0 * p.ldb);
+        const uint16_t* const a = a_of<uint16_t>(p, t.bat) + (AT ? (int64_t)t.m0 : t.m0 * p.lda);
+        const uint16_t* const b = b_of<uint16_t>(p, t.bat) + (BT ? (int64_t)t.n0 : t.n0 * p.ldb);
         char* const patch_b = lds + wave * PATCHES;
         char* const patch_a = patch_b + (BT ? kPatch : 0);
         Turn<AT, CLEAN> ta;

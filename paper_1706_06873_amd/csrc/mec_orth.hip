@@ -1,10 +1,20 @@
 // Newton-Schulz orthogonalisation of a stack of matrices: X0 = U / (|U|_F + eps), then per
-// step, with A the Gram matrix of X on its smaller side,
-//   X <- a X + (b A + c A^2) X    (rows <= cols, A = X X^T),
-//   X <- a X + X (b A + c A^2)    (else, A = X^T X),
+// step, with A the Gram matrix of X on its smaller side (m of m x n, r = n / m),
+//   X <- (a I + b A + c A^2) X    (rows <= cols, A = X X^T; else A = X^T X, from the right),
 // all in fp32 (mec_linear_f32.hip): an error of one product grows by the factor a = 3.4 per
 // step in the directions of small singular values, 140 times over the steps after the
 // first, which fp32 has room for and bf16 (2^-9 a rounding) has not.
+//
+// Several steps at once: with P = a I + b A + c A^2 the Gram matrix after the step is P A P,
+// so a phase of s steps needs one Gram matrix of X and one product with X, for Q = P_s .. P_1,
+// and the rest on m x m matrices (which commute, being polynomials of A): A^2, P A, (P A) P
+// and P Q. In products of m x m x m that is 2r + 5 against 4r + 2 for 2 steps and 2r + 9
+// against 6r + 3 for 3. The error of A is relative to its largest value, and a phase
+// multiplies it in the small singular directions, so phases are short and the longest comes
+// first, where the singular values are smallest and all still far from the polynomial's
+// range: 3 + 2 steps stay within 1.3 of the single steps' error against 64 bits (2e-6 to
+// 1.6e-5 over Gaussian, low-rank and log-spaced spectra down to 1e-6), 5 at once lose up to
+// 70 times.
 #include "mec_product.h"
 
 namespace mec {
@@ -22,13 +32,12 @@ struct OrthParams {
 };
 
 // The squares in fp64: those of gradients far from 1 leave fp32's range.
-template <class E>
-__global__ __launch_bounds__(256) void norm_squares_kernel(OrthParams p) {
-    __shared__ double sums[4];
-    const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.y * p.n;
-    const int64_t end = (blockIdx.x + 1) * p.per < p.n ? (blockIdx.x + 1) * p.per : p.n;
+template <class E, int THREADS>
+__device__ inline double sum_squares(const E* u, int64_t from, int64_t end) {
+    __shared__ double sums[THREADS / 64];
     double s = 0.0;
-    for (int64_t i = blockIdx.x * p.per + threadIdx.x; i < end; i += 256) {
+#pragma unroll 4
+    for (int64_t i = from + threadIdx.x; i < end; i += THREADS) {
         const double x = (double)to_float(u[i]);
         s += x * x;
     }
@@ -36,7 +45,18 @@ __global__ __launch_bounds__(256) void norm_squares_kernel(OrthParams p) {
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) p.part[blockIdx.y * kShares + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+    s = sums[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) s += sums[w];
+    return s;
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void norm_squares_kernel(OrthParams p) {
+    const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.y * p.n;
+    const int64_t end = (blockIdx.x + 1) * p.per < p.n ? (blockIdx.x + 1) * p.per : p.n;
+    const double s = sum_squares<E, 256>(u, blockIdx.x * p.per, end);
+    if (threadIdx.x == 0) p.part[blockIdx.y * kShares + blockIdx.x] = s;
 }
 
 template <class E>
@@ -47,115 +67,173 @@ __global__ __launch_bounds__(256) void scale_kernel(OrthParams p) {
     const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.y * p.n;
     float* const x = p.X + (int64_t)blockIdx.y * p.n;
     const int64_t end = (blockIdx.x + 1) * p.per < p.n ? (blockIdx.x + 1) * p.per : p.n;
+#pragma unroll 4
     for (int64_t i = blockIdx.x * p.per + threadIdx.x; i < end; i += 256) x[i] = (float)((double)to_float(u[i]) * by);
 }
 
-__global__ __launch_bounds__(256) void to_bf16_kernel(const float* x, uint16_t* o, int64_t n) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) o[i] = from_float<uint16_t>(x[i]);
+// small matrices: one workgroup each, in one launch
+constexpr int64_t kOneLaunch = 65536;
+template <class E>
+__global__ __launch_bounds__(1024) void norm_scale_kernel(OrthParams p) {
+    const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.x * p.n;
+    float* const x = p.X + (int64_t)blockIdx.x * p.n;
+    const double by = 1.0 / (sqrt(sum_squares<E, 1024>(u, 0, p.n)) + (double)p.eps);
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < p.n; i += 1024) x[i] = (float)((double)to_float(u[i]) * by);
+}
+
+template <class E>
+hipError_t normalise(const OrthParams& q, int32_t batch, hipStream_t stream) {
+    if (q.n <= kOneLaunch) {
+        hipLaunchKernelGGL(norm_scale_kernel<E>, dim3((uint32_t)batch), dim3(1024), 0, stream, q);
+    } else {
+        hipLaunchKernelGGL(norm_squares_kernel<E>, dim3(kShares, (uint32_t)batch), dim3(256), 0, stream, q);
+        hipLaunchKernelGGL(scale_kernel<E>, dim3(kShares, (uint32_t)batch), dim3(256), 0, stream, q);
+    }
+    return hipGetLastError();
 }
 
 int64_t round16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
+constexpr int kSquares = 7;  // m x m matrices of a phase, for each of the stack
+
+// Steps of the phase that begins with `left` steps to go.
+int32_t phase(int32_t left) { return left <= 1 ? left : left % 2 ? 3 : 2; }
+
+// A phase as its single steps, or at once: the modelled times of the products that differ.
+bool at_once_preferred(int64_t m, int64_t n, int32_t batch, int32_t steps) {
+    auto us = [&](int64_t M, int64_t N, int64_t K, int32_t b) { return plan_product(Layout::kXKt, 0, M, N, K, b, false).us; };
+    const double gram = us(m, m, n, batch), apply = us(n, m, m, batch), square = us(m, m, m, batch);
+    const double single = steps * (gram + square + apply);
+    const double at_once = gram + apply + steps * square + (steps - 1) * 2 * square +
+                           (steps > 1 ? (steps - 2) * (us(m, m, m, 2 * batch) - square) + square : 0.0);
+    return at_once < single;
+}
+
 }  // namespace
 
-// Two copies of X, A and the polynomial's matrix, and the partial norms; the output is the
-// second copy of X where it is fp32.
+// Two copies of X, the m x m matrices and the partial norms; the output is the second copy's
+// last use.
 int64_t orth_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int) {
     const int64_t m = rows < cols ? rows : cols;
-    return 16 + 2 * round16(batch * rows * cols * 4) + 2 * round16(batch * m * m * 4) + (int64_t)batch * kShares * 8;
+    return 16 + 2 * round16(batch * rows * cols * 4) + kSquares * round16(batch * m * m * 4) + (int64_t)batch * kShares * 8;
 }
 
 hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, int64_t rows, int64_t cols, int32_t steps,
                        float a, float b, float c, float eps, int dtype, hipStream_t stream) {
-    const int64_t n = rows * cols, m = rows < cols ? rows : cols;
+    const bool wide = rows <= cols;
+    const int64_t m = wide ? rows : cols, n = wide ? cols : rows, mm = m * m;
     char* at = reinterpret_cast<char*>(((uintptr_t)workspace + 15) / 16 * 16);
-    float* X[2];
-    X[0] = reinterpret_cast<float*>(at);
-    at += round16(batch * n * 4);
-    X[1] = reinterpret_cast<float*>(at);
-    at += round16(batch * n * 4);
-    float* const A = reinterpret_cast<float*>(at);
-    at += round16(batch * m * m * 4);
-    float* const P = reinterpret_cast<float*>(at);
-    at += round16(batch * m * m * 4);
+    auto take = [&](int64_t bytes) {
+        void* const p = at;
+        at += round16(bytes);
+        return static_cast<float*>(p);
+    };
+    float* const X[2] = {take(batch * m * n * 4), take(batch * m * n * 4)};
+    float* S[kSquares];
+    for (float*& s : S) s = take(batch * mm * 4);
 
     OrthParams q{};
     q.U = U;
     q.X = X[0];
     q.part = reinterpret_cast<double*>(at);
-    q.n = n;
-    q.per = (n + kShares - 1) / kShares;
+    q.n = m * n;
+    q.per = (q.n + kShares - 1) / kShares;
     q.eps = eps;
-    const dim3 grid(kShares, (uint32_t)batch);
-    if (dtype) {
-        hipLaunchKernelGGL(norm_squares_kernel<uint16_t>, grid, dim3(256), 0, stream, q);
-        hipLaunchKernelGGL(scale_kernel<uint16_t>, grid, dim3(256), 0, stream, q);
-    } else {
-        hipLaunchKernelGGL(norm_squares_kernel<float>, grid, dim3(256), 0, stream, q);
-        hipLaunchKernelGGL(scale_kernel<float>, grid, dim3(256), 0, stream, q);
-    }
-    hipError_t e = hipGetLastError();
-    for (int32_t s = 0; s < steps && e == hipSuccess; ++s) {
-        float* const from = X[s & 1];
-        float* const to = s + 1 == steps && !dtype ? static_cast<float*>(O) : X[(s + 1) & 1];
-        Product p{};
-        p.batch = batch;
-        p.splits = 1;
-        p.alpha = 1.0f;
-        // A
+    hipError_t e = dtype ? normalise<uint16_t>(q, batch, stream) : normalise<float>(q, batch, stream);
+
+    Product base{};
+    base.batch = batch;
+    base.splits = 1;
+    base.alpha = 1.0f;
+    // alpha S1 S2 of symmetric (or commuting) m x m matrices, to Y
+    auto square = [&](const float* s1, const float* s2, float* y, float alpha, const float* r, float beta, float diag) {
+        if (e != hipSuccess) return;
+        Product p = base;
+        p.A = s1;
+        p.B = s2;
+        p.Y = y;
+        p.R = r;
+        p.lda = p.ldb = p.ldy = p.ldr = m;
+        p.M = p.N = p.K = (int32_t)m;
+        p.a_batch = p.b_batch = p.y_batch = p.r_batch = mm;
+        p.alpha = alpha;
+        p.beta = beta;
+        p.diag = diag;
+        e = launch_product(Layout::kXKt, p, 0, stream);
+    };
+    int copy = 0;
+    const bool group = at_once_preferred(m, n, batch, 2);
+    for (int32_t left = steps; left > 0 && e == hipSuccess;) {
+        const int32_t now = group ? phase(left) : 1;
+        left -= now;
+        float *A = S[0], *A2 = S[1], *const T = S[2], *Q = nullptr;
+        const float* const from = X[copy];
+        Product p = base;  // A
         p.A = p.B = from;
         p.Y = A;
         p.lda = p.ldb = cols;
         p.M = p.N = (int32_t)m;
         p.ldy = m;
-        p.K = (int32_t)(n / m);
-        p.a_batch = p.b_batch = n;
-        p.y_batch = p.r_batch = m * m;
-        e = launch_product(rows <= cols ? Layout::kXKt : Layout::kXtK, p, 0, stream);
+        p.K = (int32_t)n;
+        p.a_batch = p.b_batch = m * n;
+        p.y_batch = mm;
+        e = launch_product(wide ? Layout::kXKt : Layout::kXtK, p, 0, stream);
+        for (int32_t k = 0; k < now; ++k) {
+            float* const P = S[3 + k % 2];
+            const bool last = k + 1 == now;
+            square(A, A, P, c, A, b, now > 1 ? a : 0.0f);  // the single step adds a X itself
+            if (k == 0) {
+                Q = P;
+                if (!last) square(P, A, T, 1.0f, nullptr, 0.0f, 0.0f);
+            } else if (e == hipSuccess) {
+                float* const to = S[5 + k % 2];
+                if (last) {
+                    square(P, Q, to, 1.0f, nullptr, 0.0f, 0.0f);
+                } else {  // P A and P Q in one launch
+                    p = base;
+                    p.A = P;
+                    p.B = A;
+                    p.B2 = Q;
+                    p.Y = T;
+                    p.Y2 = to;
+                    p.half = batch;
+                    p.batch = 2 * batch;
+                    p.lda = p.ldb = p.ldy = m;
+                    p.M = p.N = p.K = (int32_t)m;
+                    p.a_batch = p.b_batch = p.y_batch = mm;
+                    e = launch_product(Layout::kXKt, p, 0, stream);
+                }
+                Q = to;
+            }
+            if (!last) {
+                square(T, P, A2, 1.0f, nullptr, 0.0f, 0.0f);
+                float* const s = A;
+                A = A2;
+                A2 = s;
+            }
+        }
         if (e != hipSuccess) break;
-        // P = c A^2 + b A (A is symmetric: A A^T)
-        p.A = p.B = A;
-        p.Y = P;
-        p.R = A;
-        p.ldr = p.lda = p.ldb = m;
-        p.K = (int32_t)m;
-        p.a_batch = p.b_batch = m * m;
-        p.alpha = c;
-        p.beta = b;
-        e = launch_product(Layout::kXKt, p, 0, stream);
-        if (e != hipSuccess) break;
-        // X
-        p.alpha = 1.0f;
-        p.beta = a;
-        p.R = from;
-        p.Y = to;
+        p = base;  // X
+        if (now == 1) {
+            p.R = from;
+            p.beta = a;
+        }
+        p.Y = left ? static_cast<void*>(X[copy ^ 1]) : O;
+        p.y_bf16 = !left && dtype;
         p.M = (int32_t)rows;
         p.N = (int32_t)cols;
+        p.K = (int32_t)m;
         p.ldr = p.ldy = cols;
-        p.y_batch = p.r_batch = n;
-        if (rows <= cols) {
-            p.A = P;
-            p.lda = m;
-            p.a_batch = m * m;
-            p.B = from;
-            p.ldb = cols;
-            p.b_batch = n;
-            e = launch_product(Layout::kXK, p, 0, stream);
-        } else {
-            p.A = from;
-            p.lda = cols;
-            p.a_batch = n;
-            p.B = P;
-            p.ldb = m;
-            p.b_batch = m * m;
-            e = launch_product(Layout::kXKt, p, 0, stream);
-        }
-    }
-    if (e == hipSuccess && dtype) {
-        const int64_t total = batch * n, blocks = (total + 255) / 256;
-        hipLaunchKernelGGL(to_bf16_kernel, dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream, X[steps & 1],
-                           static_cast<uint16_t*>(O), total);
-        e = hipGetLastError();
+        p.y_batch = p.r_batch = m * n;
+        p.A = wide ? Q : from;
+        p.lda = wide ? m : cols;
+        p.a_batch = wide ? mm : m * n;
+        p.B = wide ? from : Q;
+        p.ldb = wide ? cols : m;
+        p.b_batch = wide ? m * n : mm;
+        e = launch_product(wide ? Layout::kXK : Layout::kXKt, p, 0, stream);
+        copy ^= 1;
     }
     return e;
 }

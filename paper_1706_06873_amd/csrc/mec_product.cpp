@@ -36,8 +36,7 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 
 ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split) {
     const int64_t small_rounds = ceil_div(ceil_div(M, 32) * ceil_div(N, 32) * batch, 256);
-    ProductPlan best{0, 1};
-    double best_us = (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K);
+    ProductPlan best{0, 1, (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
     const TileCost* const tiles = dtype ? kBf16 : kF32;
     const int count = dtype ? 4 : 3;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
@@ -49,10 +48,7 @@ ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
             if (real > 1) us += 3.0 + (double)(real * M * N) / 8e5;  // the sum of the shares
-            if (us < best_us) {
-                best = {i + 1, (int32_t)real};
-                best_us = us;
-            }
+            if (us < best.us) best = {i + 1, (int32_t)real, us};
         }
     }
     return best;

@@ -2,7 +2,7 @@
 // fp32): what they compute, and the epilogue that both share.
 //
 //   acc = A B, then per output (m, n), all in fp32:
-//   z = alpha*acc + bias[n] (+ beta*R[m, n] with res_first),  Z = z,
+//   z = alpha*acc + bias[n] (+ beta*R[m, n] with res_first) (+ diag where m = n),  Z = z,
 //   Y = act(z) (+ beta*R[m, n] without it)
 //
 // A is M x K, stored [m][k] or [k][m]; B is K x N, stored [n][k] or [k][n]: the layouts of
@@ -34,7 +34,12 @@ struct Product {
     int32_t splits;  // of the reduction
     int32_t batch;   // equal products, the strides below apart (elements)
     int64_t a_batch, b_batch, y_batch, r_batch;
-    int32_t symmetric;  // Y is square and symmetric (A A^T): tiles above the diagonal are mirrored
+    // half != 0: the products from `half` on take A's from the start again, and B2 and Y2
+    int32_t half;
+    const void* B2;
+    void* Y2;
+    float diag;      // added to z where m = n
+    int32_t y_bf16;  // fp32 products: Y is bf16
 
     // filled by the launch
     int32_t m_tiles, n_tiles, chunks;  // chunks of the reduction per split
@@ -46,6 +51,7 @@ struct Product {
 struct ProductPlan {
     int kernel;  // 0 the small one, from 1 the tiles
     int32_t splits;
+    double us;   // by the model
 };
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split);
 
@@ -222,6 +228,7 @@ __device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t ba
         v[e] *= p.alpha;
         if (p.bias) v[e] += p.bias[n + (e < cnt ? e : cnt - 1)];
         if (p.R && p.res_first) v[e] += p.beta * r[e];
+        if (m == n + e) v[e] += p.diag;
     }
     auto store = [&](void* base, int64_t at) {
         E* const to = static_cast<E*>(base) + at;
@@ -249,7 +256,26 @@ __device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t ba
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += p.beta * r[e];
     }
-    store(p.Y, bat * p.y_batch + m * p.ldy + n);
+    void* const Y = p.half && bat >= p.half ? p.Y2 : p.Y;
+    const int64_t at = (p.half && bat >= p.half ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
+    if (sizeof(E) == 4 && p.y_bf16) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e < cnt) static_cast<uint16_t*>(Y)[at + e] = from_float<uint16_t>(v[e]);
+    } else {
+        store(Y, at);
+    }
+}
+
+// the operands of product `bat` of a batch
+template <class E>
+__device__ inline const E* a_of(const Product& p, int32_t bat) {
+    return static_cast<const E*>(p.A) + (p.half && bat >= p.half ? bat - p.half : bat) * p.a_batch;
+}
+template <class E>
+__device__ inline const E* b_of(const Product& p, int32_t bat) {
+    return p.half && bat >= p.half ? static_cast<const E*>(p.B2) + (bat - p.half) * p.b_batch
+                                   : static_cast<const E*>(p.B) + bat * p.b_batch;
 }
 
 // A wave's BM x BN blocks of 32 x 32 sums, as the products leave them with B's columns as
