@@ -17,20 +17,21 @@
 namespace mec {
 namespace {
 
-constexpr int kKT = 64;  // chunk of the reduction
-
-template <int BM, int BN, int WM, int WN, Layout L, bool DMA>
+// BM x BN 32 x 32 blocks per wave, WM x WN waves, chunks of KT, S stages of LDS (DMA).
+template <int BM, int BN, int WM, int WN, int KT, int S, Layout L, bool DMA>
 struct Cfg {
+    static constexpr int kKT = KT, kS = DMA ? S : 2;
     static constexpr int kBM = BM, kBN = BN, kWM = WM, kWN = WN;
     static constexpr bool kAT = L == Layout::kXtK;   // A stored [k][m]
     static constexpr bool kBT = L != Layout::kXKt;   // B stored [k][n]
     static constexpr bool kDMA = DMA;
     static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int AB = TM * kKT * 2, BB = TN * kKT * 2, STAGE = AB + BB;  // bytes
-    static constexpr int AI = TM * 8 / THREADS, BI = TN * 8 / THREADS;           // granules per thread
+    static constexpr int kLoads = (TM + TN) * (KT / 8) / THREADS;                // granules per thread
     static constexpr int EPI = WAVES * 32 * (32 * BN + 4) * 4;
-    static constexpr int LDS = 2 * STAGE > EPI ? 2 * STAGE : EPI;
-    static_assert(TM * 8 % THREADS == 0 && TN * 8 % THREADS == 0 && LDS <= 160 * 1024, "tile");
+    static constexpr int LDS = kS * STAGE > EPI ? kS * STAGE : EPI;
+    static_assert(TM * (KT / 8) % THREADS == 0 && TN * (KT / 8) % THREADS == 0 && LDS <= 160 * 1024, "tile");
+    static_assert((kS - 2) * kLoads < 64, "loads in flight");
 };
 
 __device__ inline uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -59,9 +60,10 @@ __device__ inline void to_lds16(u32x4v rsrc, uint32_t voff, uint32_t lds) {
 
 // One operand's T rows (stored along the reduction) or columns (TR: across it) of a tile.
 // WIDE items of 16 bytes per thread.
-template <int T, int THREADS, bool TR, bool DMA>
+template <int T, int THREADS, int KT, bool TR, bool DMA>
 struct Operand {
-    static constexpr int ITEMS = T * 8 / THREADS;
+    static constexpr int G = KT / 8;  // granules along a chunk
+    static constexpr int ITEMS = T * G / THREADS;
     static constexpr int SW = T / 16 < 8 ? T / 16 - 1 : 7;
     const char* base;   // uniform: the tile's first row and the chunk's first k
     int64_t step;       // bytes from chunk to chunk
@@ -71,6 +73,8 @@ struct Operand {
     int32_t have;       // TR: columns from this thread's on; else 8 k of this thread's granule start here
     int32_t k_at;       // else: first k of this thread's granule
 
+    static __device__ inline int swizzle(int row) { return KT == 64 ? row & 7 : (row >> 1) & 3; }
+
     // rows r0 .. of `count` rows (columns) of `ld` elements, reduction from k0 to k1
     __device__ inline void init(const void* mem, int64_t ld_, int32_t r0, int32_t count, int64_t k0, int64_t k1, int tid) {
         ld = ld_;
@@ -78,7 +82,7 @@ struct Operand {
             const int pos = tid % (T / 8), k = tid / (T / 8);
             const int col = (((pos >> 1) ^ (k & SW)) * 2 + (pos & 1)) * 8;
             base = scalar(static_cast<const char*>(mem) + 2 * (k0 * ld + r0));
-            step = 2 * kKT * ld;
+            step = 2 * KT * ld;
             have = count - r0 - col;
             k_at = k;
             if constexpr (DMA) {
@@ -92,14 +96,14 @@ struct Operand {
                 left = k1 - k0;
             }
         } else {
-            const int row = tid / 8, kg = (tid % 8) ^ (row & 7);
+            const int row = tid / G, kg = (tid % G) ^ swizzle(row);
             base = scalar(static_cast<const char*>(mem) + 2 * (r0 * ld + k0));
-            step = 2 * kKT;
+            step = 2 * KT;
             left = k1 - k0;
             k_at = 8 * kg;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                int r = row + i * (THREADS / 8);
+                int r = row + i * (THREADS / G);
                 if (r0 + r >= count) r = count - 1 - r0;  // rows past the last are not stored
                 voff[i] = DMA ? 2u * (uint32_t)(r * ld + 8 * kg) : (uint32_t)r;
             }
@@ -107,7 +111,7 @@ struct Operand {
     }
     __device__ inline void next() {
         base += step;
-        left -= TR && DMA ? step : kKT;
+        left -= TR && DMA ? step : KT;
     }
     // DMA: this chunk to LDS at `to`
     __device__ inline void stage(uint32_t to, int wave) const {
@@ -152,16 +156,16 @@ struct Operand {
             return join_tr(h[0], h[1]);
         } else {
             const int r = blk * 32 + (lane & 31), g = 2 * kk + (lane >> 5);
-            return *reinterpret_cast<const bf16x8*>(from + r * 128 + ((g ^ (r & 7)) << 4));
+            return *reinterpret_cast<const bf16x8*>(from + r * (KT * 2) + ((g ^ swizzle(r)) << 4));
         }
     }
 };
 
 template <class C>
 __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
-    constexpr int BM = C::kBM, BN = C::kBN;
-    using OpA = Operand<C::TM, C::THREADS, C::kAT, C::kDMA>;
-    using OpB = Operand<C::TN, C::THREADS, C::kBT, C::kDMA>;
+    constexpr int BM = C::kBM, BN = C::kBN, KT = C::kKT;
+    using OpA = Operand<C::TM, C::THREADS, C::kKT, C::kAT, C::kDMA>;
+    using OpB = Operand<C::TN, C::THREADS, C::kKT, C::kBT, C::kDMA>;
     __shared__ __align__(16) char lds[C::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = (int)scalar((uint32_t)tid >> 6);
     const int wm = wave % C::kWM, wn = wave / C::kWM;
@@ -171,9 +175,9 @@ __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
     uint32_t mt, nt;
     tile_of(b - split * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
     const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
-    const int64_t k0 = (int64_t)split * p.chunks * kKT;
-    const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
-    const int chunks = (int)((k1 - k0 + kKT - 1) / kKT);
+    const int64_t k0 = (int64_t)split * p.chunks * KT;
+    const int64_t k1 = k0 + (int64_t)p.chunks * KT < p.K ? k0 + (int64_t)p.chunks * KT : p.K;
+    const int chunks = (int)((k1 - k0 + KT - 1) / KT);
 
     OpA a;
     OpB bb;
@@ -182,36 +186,87 @@ __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
     const uint32_t at = (uint32_t)(uintptr_t)(lds_char*)lds;
 
     floatx16 acc[BM][BN] = {};
+    struct Frags {
+        bf16x8 a[BM], b[BN];
+    };
+    auto read = [&](Frags& f, const char* from, int kk) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i) f.a[i] = OpA::frag(from, wm * BM + i, kk, lane);
+#pragma unroll
+        for (int j = 0; j < BN; ++j) f.b[j] = OpB::frag(from + C::AB, wn * BN + j, kk, lane);
+    };
+    auto multiply = [&](const Frags& f) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
+    };
     auto products = [&](const char* from) {
 #pragma unroll
-        for (int kk = 0; kk < kKT / 16; ++kk) {
-            bf16x8 fa[BM], fb[BN];
-#pragma unroll
-            for (int i = 0; i < BM; ++i) fa[i] = OpA::frag(from, wm * BM + i, kk, lane);
-#pragma unroll
-            for (int j = 0; j < BN; ++j) fb[j] = OpB::frag(from + C::AB, wn * BN + j, kk, lane);
-#pragma unroll
-            for (int i = 0; i < BM; ++i)
-#pragma unroll
-                for (int j = 0; j < BN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        for (int kk = 0; kk < KT / 16; ++kk) {
+            Frags f;
+            read(f, from, kk);
+            multiply(f);
         }
     };
-    if constexpr (C::kDMA) {
-        a.stage(at, wave);
-        bb.stage(at + C::AB, wave);
+    auto stage = [&](uint32_t to) {
+        a.stage(at + to, wave);
+        bb.stage(at + to + C::AB, wave);
+        a.next();
+        bb.next();
+    };
+    if constexpr (C::kDMA && C::kS > 2) {
+        // S - 1 chunks on their way; those past the last are zeros, so that the loads in
+        // flight stay the same number. Fragments are read one step of 16 k ahead of their
+        // products, across the chunks' borders too.
+        constexpr int S = C::kS, STEPS = KT / 16;
+        uint32_t now = 0, then = (S - 1) * C::STAGE;
+        auto after = [&](uint32_t x) { return x + C::STAGE == S * C::STAGE ? 0u : x + C::STAGE; };
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) stage(s * C::STAGE);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * C::kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        Frags f[2];
+        read(f[0], lds, 0);
+        static_assert(STEPS % 2 == 0, "the first fragments of a chunk go to f[0]");
+        for (int c = 0; c < chunks; ++c) {
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk) {
+                if (kk + 1 < STEPS) {
+                    read(f[(kk + 1) % 2], lds + now, kk + 1);
+                } else {
+                    // the next chunk has arrived for every wave, and none reads the last one's
+                    // stage any more: its fragments went into products before this chunk's
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 3) * C::kLoads) : "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    now = after(now);
+                    read(f[(kk + 1) % 2], lds + now, 0);
+                    stage(then);
+                    then = after(then);
+                }
+                multiply(f[kk % 2]);
+                if constexpr (BM * BN > 1) {
+#pragma unroll
+                    for (int g = 0; g < BM * BN; ++g) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    } else if constexpr (C::kDMA) {
+        stage(0);
         for (int c = 0; c < chunks; ++c) {
             const uint32_t now = (c & 1) * C::STAGE, then = C::STAGE - now;
             // this chunk has arrived for every wave, and none reads the other stage any more
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (c + 1 < chunks) {
-                a.next();
-                bb.next();
-                a.stage(at + then, wave);
-                bb.stage(at + then + C::AB, wave);
-            }
+            if (c + 1 < chunks) stage(then);
             products(lds + now);
         }
     } else {
@@ -242,19 +297,20 @@ __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
     epilogue<uint16_t, BM, BN>(p, acc, mine, m0 + wm * BM * 32, n0 + wn * BN * 32, 0, (int32_t)split, lane);
 }
 
-template <int BM, int BN, int WM, int WN, Layout L>
+template <int BM, int BN, int WM, int WN, int KT, int S, Layout L>
 hipError_t run(Product p, hipStream_t stream) {
-    using C = Cfg<BM, BN, WM, WN, L, true>;
+    using C = Cfg<BM, BN, WM, WN, KT, S, L, true>;
     p.m_tiles = (p.M + C::TM - 1) / C::TM;
     p.n_tiles = (p.N + C::TN - 1) / C::TN;
-    const int64_t chunks = ((int64_t)p.K + kKT - 1) / kKT;
-    p.chunks = (int32_t)((chunks + p.splits - 1) / p.splits);
+    // shares are whole multiples of 64 elements
+    const int64_t chunks = 64 / KT * (((int64_t)p.K + 63) / 64);
+    p.chunks = 64 / KT * (int32_t)((chunks / (64 / KT) + p.splits - 1) / p.splits);
     const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * p.splits;
     if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
     if (p.clean) {
         hipLaunchKernelGGL(product_bf16_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
     } else {
-        using G = Cfg<BM, BN, WM, WN, L, false>;
+        using G = Cfg<BM, BN, WM, WN, KT, S, L, false>;
         hipLaunchKernelGGL(product_bf16_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
     }
     return hipGetLastError();
@@ -263,10 +319,11 @@ hipError_t run(Product p, hipStream_t stream) {
 template <Layout L>
 hipError_t pick(const Product& p, int tile, hipStream_t stream) {
     switch (tile) {
-        case 1: return run<2, 2, 2, 2, L>(p, stream);
-        case 2: return run<4, 2, 2, 4, L>(p, stream);
-        case 3: return run<1, 2, 2, 2, L>(p, stream);
-        case 4: return run<1, 1, 2, 2, L>(p, stream);
+        case 1: return run<2, 2, 2, 2, 64, 2, L>(p, stream);
+        case 2: return run<4, 2, 2, 4, 32, 4, L>(p, stream);
+        case 3: return run<1, 2, 2, 2, 64, 2, L>(p, stream);
+        case 4: return run<1, 1, 2, 2, 64, 2, L>(p, stream);
+        case 5: return run<1, 1, 2, 2, 64, 4, L>(p, stream);
         default: return hipErrorNotSupported;
     }
 }

@@ -185,8 +185,9 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
         MEC_MM(0, 2, low)
 #undef MEC_MM
     };
-    // One chunk at a time in registers: it is requested under the second half of the chunk
-    // before the last and split into the other stage under the first half of the last.
+    // One chunk at a time in registers: it is requested under the second half of a chunk's
+    // products and split into the other stage under the first half of the next one's. (Two and
+    // four chunks in registers: 1024 x 1024 x 1024 in 64 x 64 tiles 25.5 us, 29.2, 39.7.)
     Frags f;
     Regs r;
     load(r);

@@ -17,10 +17,11 @@ struct TileCost {
     double chunk[5], ends;
 };
 // by the kernels' numbers, from 1
-constexpr TileCost kBf16[] = {{128, 128, 2, {0.60, 0.93}, 6.0},
-                              {256, 256, 1, {1.55}, 12.0},
-                              {64, 128, 3, {0.42, 0.65, 0.80}, 4.8},
-                              {64, 64, 5, {0.30, 0.47, 0.62, 0.78, 0.87}, 3.7}};
+constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
+                              {256, 256, 1, {1.45}, 8.5},
+                              {64, 128, 3, {0.40, 0.70, 0.85}, 3.5},
+                              {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4},
+                              {64, 64, 2, {0.26, 0.38}, 3.8}};
 constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 7.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -38,7 +39,7 @@ ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int
     const int64_t small_rounds = ceil_div(ceil_div(M, 32) * ceil_div(N, 32) * batch, 256);
     ProductPlan best{0, 1, (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
     const TileCost* const tiles = dtype ? kBf16 : kF32;
-    const int count = dtype ? 4 : 3;
+    const int count = dtype ? 5 : 3;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
     for (int i = 0; i < count; ++i) {
         const int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn) * batch;

@@ -278,32 +278,131 @@ __device__ inline const E* b_of(const Product& p, int32_t bat) {
                                    : static_cast<const E*>(p.B) + bat * p.b_batch;
 }
 
+// 8 elements as they lie in memory
+template <class E>
+struct Pack8 {
+    u32x4v w[sizeof(E) / 2];
+    __device__ inline void load(const E* src) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(E) / 2; ++i) w[i] = reinterpret_cast<const u32x4v*>(src)[i];
+    }
+    __device__ inline float get(int e) const {
+        if constexpr (sizeof(E) == 4) {
+            return __builtin_bit_cast(float, (uint32_t)w[e / 4][e % 4]);
+        } else {
+            const uint32_t x = w[0][e / 2];
+            return __builtin_bit_cast(float, e % 2 ? x & 0xffff0000u : x << 16);
+        }
+    }
+};
+
 // A wave's BM x BN blocks of 32 x 32 sums, as the products leave them with B's columns as
 // the instruction's rows (lane l holds m = l % 32 and, in register v, n = acc_row(v, l)),
 // through `mine`, 32 rows of 32*BN + 4 floats of LDS that only this wave uses: rows are
-// read back whole, so that Y, Z and R move in runs of 64*BN (bf16) or 128*BN bytes.
+// read back whole, so that Y, Z and R move in runs of 64*BN (bf16) or 128*BN bytes. Blocks
+// that lie inside Y, with 16-byte rows, take the first path, whose loads and LDS reads of 32
+// rows are all in flight at once (8192 x 8192 x 64 in bf16: 60 us with the second path alone).
 template <class E, int BM, int BN>
 __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN], float* mine, int32_t m0, int32_t n0,
                                 int32_t bat, int32_t split, int lane) {
-    constexpr int PITCH = 32 * BN + 4, LPR = 4 * BN, RPP = 64 / LPR;
+    constexpr int PITCH = 32 * BN + 4, LPR = 4 * BN, RPP = 64 / LPR, PASSES = 32 / RPP;
+    constexpr bool FAST = sizeof(E) == 2;
+    const int row0 = lane / LPR, col = (lane % LPR) * 8;
+    const bool inside = p.vec && m0 + 32 * BM <= p.M && n0 + 32 * BN <= p.N && !p.y_bf16;
+    const bool part = p.splits > 1, diagonal = p.diag != 0.0f;
+    const bool second = p.half && bat >= p.half;
+    float bias[8] = {};
+    E* y = nullptr;
+    E* z = nullptr;
+    const E* r = nullptr;
+    float* q = nullptr;
+    if (inside) {
+        const int64_t m = m0 + row0;
+        if (part) {
+            q = p.part + ((int64_t)split * p.M + m) * p.N + n0 + col;
+        } else {
+            y = static_cast<E*>(second ? p.Y2 : p.Y) + (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n0 + col;
+            if (p.Z) z = static_cast<E*>(p.Z) + m * p.ldz + n0 + col;
+            if (p.R) r = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n0 + col;
+            if (p.bias)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bias[e] = p.bias[n0 + col + e];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
+        Pack8<E> rr[PASSES];
+        if (r)
+#pragma unroll
+            for (int s = 0; s < PASSES; ++s) rr[s].load(r + (i * 32 + s * RPP) * p.ldr);
         asm volatile("" ::: "memory");  // the wave's LDS accesses stay in this order
 #pragma unroll
         for (int j = 0; j < BN; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4v*>(mine + (lane & 31) * PITCH + j * 32 + q * 8 + (lane >> 5) * 4) =
-                    f32x4v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f32x4v*>(mine + (lane & 31) * PITCH + j * 32 + k * 8 + (lane >> 5) * 4) =
+                    f32x4v{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
+        if (inside) {
+            float v[PASSES][8];
+#pragma unroll
+            for (int s = 0; s < PASSES; ++s) load8v(mine + (s * RPP + row0) * PITCH + col, v[s]);
+            if (part) {
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s) store8v(q + (int64_t)(i * 32 + s * RPP) * p.N, v[s]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[s][e] = v[s][e] * p.alpha + bias[e];
+                if (r && p.res_first)
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
+                if (diagonal)
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (m0 + i * 32 + s * RPP + row0 == n0 + col + e) v[s][e] += p.diag;
+                if (z)
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s) store8v(z + (i * 32 + s * RPP) * p.ldz, v[s]);
+                if (p.act == kActRelu) {
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActRelu, v[s][e]);
+                } else if (p.act == kActSilu) {
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActSilu, v[s][e]);
+                } else if (p.act == kActGelu) {
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActGelu, v[s][e]);
+                }
+                if (r && !p.res_first)
+#pragma unroll
+                    for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s) store8v(y + (i * 32 + s * RPP) * p.ldy, v[s]);
+            }
+        } else {
 #pragma unroll 1
-        for (int s = 0; s < 32 / RPP; ++s) {
-            const int row = s * RPP + lane / LPR, col = (lane % LPR) * 8;
-            float v[8];
-            load8v(mine + row * PITCH + col, v);
-            const int32_t m = m0 + i * 32 + row, n = n0 + col;
-            if (m < p.M && n < p.N) finish<E, 8>(p, m, n, bat, split, v);
+            for (int s = 0; s < PASSES; ++s) {
+                const int row = s * RPP + row0;
+                float v[8];
+                load8v(mine + row * PITCH + col, v);
+                const int32_t m = m0 + i * 32 + row, n = n0 + col;
+                if (m < p.M && n < p.N) finish<E, 8>(p, m, n, bat, split, v);
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
