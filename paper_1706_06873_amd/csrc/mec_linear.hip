@@ -332,7 +332,6 @@ hipError_t pick(const Product& p, int tile, hipStream_t stream) {
 
 hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream) {
     auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 8 == 0); };
-    p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0;
     // the dimension that each operand's rows run along has to be whole granules
     const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
     p.clean = rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;

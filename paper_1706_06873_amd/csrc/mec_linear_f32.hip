@@ -276,9 +276,6 @@ hipError_t pick(const Product& p, int tile, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream) {
-    auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 4 == 0); };
-    p.vec = p.N % 8 == 0 && rows16(p.Y, p.ldy) && rows16(p.Z, p.ldz) && rows16(p.R, p.ldr) && ((uintptr_t)p.part & 15u) == 0 &&
-            p.y_batch % 4 == 0 && p.r_batch % 4 == 0;
     switch (layout) {
         case Layout::kXK: return pick<Layout::kXK>(p, tile, stream);
         case Layout::kXKt: return pick<Layout::kXKt>(p, tile, stream);

@@ -32,9 +32,9 @@ __device__ inline void join(const Product& p, const floatx16& acc, float* sums, 
     __syncthreads();
     const int m = (int)threadIdx.x / 32, n = (int)threadIdx.x % 32;
     if (m0 + m >= p.M || n0 + n >= p.N) return;
-    float v[1] = {0.0f};
-    for (int w = 0; w < waves; ++w) v[0] += sums[w * 32 * kPitch + m * kPitch + n];
-    finish<E, 1>(p, m0 + m, n0 + n, bat, 0, v);
+    float v = 0.0f;
+    for (int w = 0; w < waves; ++w) v += sums[w * 32 * kPitch + m * kPitch + n];
+    finish<E>(p, m0 + m, n0 + n, bat, v);
 }
 
 struct Place {

@@ -43,7 +43,6 @@ struct Product {
 
     // filled by the launch
     int32_t m_tiles, n_tiles, chunks;  // chunks of the reduction per split
-    int32_t vec;                       // 16-byte rows of Y, Z and R, 16-byte partial sums
     int32_t clean;                     // 16-byte rows of A and B
 };
 
@@ -198,73 +197,24 @@ __device__ inline bf16x8 join_tr(s16x4 a, s16x4 b) {
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// V outputs (m, n .. n + V - 1) from their sums v
-template <class E, int V>
-__device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t bat, int32_t split, float* v) {
-    const int cnt = p.N - n < V ? p.N - n : V;
-    if (p.splits > 1) {
-        float* const to = p.part + ((int64_t)split * p.M + m) * p.N + n;
-        if (V == 8 && p.vec) {
-            store8v(to, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (e < cnt) to[e] = v[e];
-        }
-        return;
-    }
-    float r[V] = {};
-    if (p.R) {
-        const E* const from = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;
-        if (V == 8 && p.vec) {
-            load8v(from, r);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) r[e] = e < cnt ? to_float(from[e]) : 0.0f;
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        v[e] *= p.alpha;
-        if (p.bias) v[e] += p.bias[n + (e < cnt ? e : cnt - 1)];
-        if (p.R && p.res_first) v[e] += p.beta * r[e];
-        if (m == n + e) v[e] += p.diag;
-    }
-    auto store = [&](void* base, int64_t at) {
-        E* const to = static_cast<E*>(base) + at;
-        if (V == 8 && p.vec) {
-            store8v(to, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (e < cnt) to[e] = from_float<E>(v[e]);
-        }
-    };
-    if (p.Z) store(p.Z, m * p.ldz + n);
+// one output (m, n) from its sum v
+template <class E>
+__device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t bat, float v) {
     constexpr bool FAST = sizeof(E) == 2;
-    if (p.act == kActRelu) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActRelu, v[e]);
-    } else if (p.act == kActSilu) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActSilu, v[e]);
-    } else if (p.act == kActGelu) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = act_value<FAST>(kActGelu, v[e]);
-    }
-    if (p.R && !p.res_first) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] += p.beta * r[e];
-    }
-    void* const Y = p.half && bat >= p.half ? p.Y2 : p.Y;
-    const int64_t at = (p.half && bat >= p.half ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
-    if (sizeof(E) == 4 && p.y_bf16) {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (e < cnt) static_cast<uint16_t*>(Y)[at + e] = from_float<uint16_t>(v[e]);
-    } else {
-        store(Y, at);
-    }
+    const float r = p.R ? p.beta * to_float(static_cast<const E*>(p.R)[bat * p.r_batch + m * p.ldr + n]) : 0.0f;
+    v *= p.alpha;
+    if (p.bias) v += p.bias[n];
+    if (p.R && p.res_first) v += r;
+    if (m == n) v += p.diag;
+    if (p.Z) static_cast<E*>(p.Z)[m * p.ldz + n] = from_float<E>(v);
+    if (p.act == kActRelu) v = act_value<FAST>(kActRelu, v);
+    else if (p.act == kActSilu) v = act_value<FAST>(kActSilu, v);
+    else if (p.act == kActGelu) v = act_value<FAST>(kActGelu, v);
+    if (p.R && !p.res_first) v += r;
+    const bool second = p.half && bat >= p.half;
+    const int64_t at = (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
+    if (sizeof(E) == 4 && p.y_bf16) static_cast<uint16_t*>(p.Y)[at] = from_float<uint16_t>(v);
+    else static_cast<E*>(second ? p.Y2 : p.Y)[at] = from_float<E>(v);
 }
 
 // the operands of product `bat` of a batch
@@ -278,13 +228,41 @@ __device__ inline const E* b_of(const Product& p, int32_t bat) {
                                    : static_cast<const E*>(p.B) + bat * p.b_batch;
 }
 
-// 8 elements as they lie in memory
+// 8 elements as they lie in memory, at any boundary of the element's size
 template <class E>
 struct Pack8 {
-    u32x4v w[sizeof(E) / 2];
-    __device__ inline void load(const E* src) {
+    static constexpr int W = sizeof(E) / 2;
+    struct __attribute__((packed, aligned(sizeof(E)))) Any {
+        u32x4v v;
+    };
+    u32x4v w[W];
+    // the first `have` of them
+    __device__ inline void load(const E* src, int have) {
+        if (have >= 8) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(E) / 2; ++i) w[i] = reinterpret_cast<const u32x4v*>(src)[i];
+            for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const Any*>(src)[i].v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < have) set(e, src[e]);
+        }
+    }
+    __device__ inline void store(E* dst, int have) const {
+        if (have >= 8) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) reinterpret_cast<Any*>(dst)[i].v = w[i];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < have) {
+                    if constexpr (sizeof(E) == 4) dst[e] = __builtin_bit_cast(float, (uint32_t)w[e / 4][e % 4]);
+                    else dst[e] = (E)(w[0][e / 2] >> (16 * (e % 2)));
+                }
+        }
+    }
+    __device__ inline void set(int e, E x) {
+        if constexpr (sizeof(E) == 4) w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, x);
+        else w[0][e / 2] = e % 2 ? (w[0][e / 2] & 0xffffu) | (uint32_t)x << 16 : (w[0][e / 2] & 0xffff0000u) | x;
     }
     __device__ inline float get(int e) const {
         if constexpr (sizeof(E) == 4) {
@@ -294,47 +272,52 @@ struct Pack8 {
             return __builtin_bit_cast(float, e % 2 ? x & 0xffff0000u : x << 16);
         }
     }
+    __device__ inline void round(const float* v) {
+        if constexpr (sizeof(E) == 4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[0][e] = (uint32_t)from_float<uint16_t>(v[2 * e]) | (uint32_t)from_float<uint16_t>(v[2 * e + 1]) << 16;
+        }
+    }
 };
 
 // A wave's BM x BN blocks of 32 x 32 sums, as the products leave them with B's columns as
 // the instruction's rows (lane l holds m = l % 32 and, in register v, n = acc_row(v, l)),
 // through `mine`, 32 rows of 32*BN + 4 floats of LDS that only this wave uses: rows are
-// read back whole, so that Y, Z and R move in runs of 64*BN (bf16) or 128*BN bytes. Blocks
-// that lie inside Y, with 16-byte rows, take the first path, whose loads and LDS reads of 32
-// rows are all in flight at once (8192 x 8192 x 64 in bf16: 60 us with the second path alone).
+// read back whole, so that Y, Z and R move in runs of 64*BN (bf16) or 128*BN bytes. The
+// loads and LDS reads of 32 rows are all in flight at once (8192 x 8192 x 64 in bf16 37 us;
+// 60 with 8 rows after another).
 template <class E, int BM, int BN>
 __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN], float* mine, int32_t m0, int32_t n0,
                                 int32_t bat, int32_t split, int lane) {
     constexpr int PITCH = 32 * BN + 4, LPR = 4 * BN, RPP = 64 / LPR, PASSES = 32 / RPP;
     constexpr bool FAST = sizeof(E) == 2;
     const int row0 = lane / LPR, col = (lane % LPR) * 8;
-    const bool inside = p.vec && m0 + 32 * BM <= p.M && n0 + 32 * BN <= p.N && !p.y_bf16;
-    const bool part = p.splits > 1, diagonal = p.diag != 0.0f;
-    const bool second = p.half && bat >= p.half;
+    const int32_t have = p.N - n0 - col;  // columns from this lane's first on
+    const int32_t rows = p.M - m0 - row0;
+    const bool part = p.splits > 1, diagonal = p.diag != 0.0f, second = p.half && bat >= p.half;
+    const bool half = sizeof(E) == 4 && p.y_bf16;
+    const int64_t m = m0 + row0, n = n0 + col;
+    const int64_t yat = (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
+    E* const y = static_cast<E*>(second ? p.Y2 : p.Y) + yat;
+    uint16_t* const y16 = static_cast<uint16_t*>(p.Y) + yat;
+    E* const z = static_cast<E*>(p.Z) + m * p.ldz + n;
+    const E* const r = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;
+    float* const q = p.part + ((int64_t)split * p.M + m) * p.N + n;
     float bias[8] = {};
-    E* y = nullptr;
-    E* z = nullptr;
-    const E* r = nullptr;
-    float* q = nullptr;
-    if (inside) {
-        const int64_t m = m0 + row0;
-        if (part) {
-            q = p.part + ((int64_t)split * p.M + m) * p.N + n0 + col;
-        } else {
-            y = static_cast<E*>(second ? p.Y2 : p.Y) + (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n0 + col;
-            if (p.Z) z = static_cast<E*>(p.Z) + m * p.ldz + n0 + col;
-            if (p.R) r = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n0 + col;
-            if (p.bias)
+    if (p.bias && !part)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) bias[e] = p.bias[n0 + col + e];
-        }
-    }
+        for (int e = 0; e < 8; ++e) bias[e] = e < have ? p.bias[n + e] : 0.0f;
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
         Pack8<E> rr[PASSES];
-        if (r)
+        if (p.R && !part)
 #pragma unroll
-            for (int s = 0; s < PASSES; ++s) rr[s].load(r + (i * 32 + s * RPP) * p.ldr);
+            for (int s = 0; s < PASSES; ++s)
+                if (i * 32 + s * RPP < rows) rr[s].load(r + (i * 32 + s * RPP) * p.ldr, have);
         asm volatile("" ::: "memory");  // the wave's LDS accesses stay in this order
 #pragma unroll
         for (int j = 0; j < BN; ++j)
@@ -344,65 +327,73 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
                     f32x4v{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
-        if (inside) {
-            float v[PASSES][8];
+        float v[PASSES][8];
 #pragma unroll
-            for (int s = 0; s < PASSES; ++s) load8v(mine + (s * RPP + row0) * PITCH + col, v[s]);
-            if (part) {
+        for (int s = 0; s < PASSES; ++s) load8v(mine + (s * RPP + row0) * PITCH + col, v[s]);
+        if (part) {
 #pragma unroll
-                for (int s = 0; s < PASSES; ++s) store8v(q + (int64_t)(i * 32 + s * RPP) * p.N, v[s]);
-            } else {
+            for (int s = 0; s < PASSES; ++s) {
+                Pack8<float> o;
+                o.round(v[s]);
+                if (i * 32 + s * RPP < rows) o.store(q + (int64_t)(i * 32 + s * RPP) * p.N, have);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[s][e] = v[s][e] * p.alpha + bias[e];
+            if (p.R && p.res_first)
 #pragma unroll
                 for (int s = 0; s < PASSES; ++s)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[s][e] = v[s][e] * p.alpha + bias[e];
-                if (r && p.res_first)
+                    for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
+            if (diagonal)
 #pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
+                for (int s = 0; s < PASSES; ++s)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
-                if (diagonal)
+                    for (int e = 0; e < 8; ++e)
+                        if (m0 + i * 32 + s * RPP + row0 == n0 + col + e) v[s][e] += p.diag;
+            if (p.Z)
 #pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (m0 + i * 32 + s * RPP + row0 == n0 + col + e) v[s][e] += p.diag;
-                if (z)
-#pragma unroll
-                    for (int s = 0; s < PASSES; ++s) store8v(z + (i * 32 + s * RPP) * p.ldz, v[s]);
-                if (p.act == kActRelu) {
-#pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActRelu, v[s][e]);
-                } else if (p.act == kActSilu) {
-#pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActSilu, v[s][e]);
-                } else if (p.act == kActGelu) {
-#pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActGelu, v[s][e]);
+                for (int s = 0; s < PASSES; ++s) {
+                    Pack8<E> o;
+                    o.round(v[s]);
+                    if (i * 32 + s * RPP < rows) o.store(z + (i * 32 + s * RPP) * p.ldz, have);
                 }
-                if (r && !p.res_first)
+            if (p.act == kActRelu) {
 #pragma unroll
-                    for (int s = 0; s < PASSES; ++s)
+                for (int s = 0; s < PASSES; ++s)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
+                    for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActRelu, v[s][e]);
+            } else if (p.act == kActSilu) {
 #pragma unroll
-                for (int s = 0; s < PASSES; ++s) store8v(y + (i * 32 + s * RPP) * p.ldy, v[s]);
+                for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActSilu, v[s][e]);
+            } else if (p.act == kActGelu) {
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[s][e] = act_value<FAST>(kActGelu, v[s][e]);
             }
-        } else {
-#pragma unroll 1
-            for (int s = 0; s < PASSES; ++s) {
-                const int row = s * RPP + row0;
-                float v[8];
-                load8v(mine + row * PITCH + col, v);
-                const int32_t m = m0 + i * 32 + row, n = n0 + col;
-                if (m < p.M && n < p.N) finish<E, 8>(p, m, n, bat, split, v);
-            }
+            if (p.R && !p.res_first)
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[s][e] += p.beta * rr[s].get(e);
+#pragma unroll
+            for (int s = 0; s < PASSES; ++s)
+                if (i * 32 + s * RPP < rows) {
+                    if (half) {
+                        Pack8<uint16_t> o;
+                        o.round(v[s]);
+                        o.store(y16 + (i * 32 + s * RPP) * p.ldy, have);
+                    } else {
+                        Pack8<E> o;
+                        o.round(v[s]);
+                        o.store(y + (i * 32 + s * RPP) * p.ldy, have);
+                    }
+                }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
