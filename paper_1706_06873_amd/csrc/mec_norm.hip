@@ -30,27 +30,48 @@ struct NormParams {
     float eps;
 };
 
-// V consecutive elements as floats
+// V consecutive elements (16 bytes' worth) at any boundary of the element's size, of which
+// `have` are the row's; the others come as zeros and are not written. (The same instructions
+// as for 16-byte rows; single elements took 725 us where these take 180, 108934 rows of 1619
+// in bf16.)
+struct __attribute__((packed, aligned(4))) AnyF {
+    f32x4v v;
+};
 template <int V, class E>
-__device__ inline void load_v(const E* src, float* v) {
-    if constexpr (V == 8) {
-        load8v(src, v);
-    } else if constexpr (V == 4) {
-        const f32x4v w = *reinterpret_cast<const f32x4v*>(src);
+__device__ inline void load_v(const E* src, int have, float* v) {
+    if constexpr (sizeof(E) == 2) {
+        static_assert(V == 8, "16 bytes");
+        const u32x4v w = load_some(src, have);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = w[e];
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+        }
+    } else if (have >= V) {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            const f32x4v w = reinterpret_cast<const AnyF*>(src + h)->v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[h + e] = w[e];
+        }
     } else {
-        v[0] = to_float(src[0]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = e < have ? src[e] : 0.0f;
     }
 }
 template <int V, class E>
-__device__ inline void store_v(E* dst, const float* v) {
-    if constexpr (V == 8) {
-        store8v(dst, v);
-    } else if constexpr (V == 4) {
-        *reinterpret_cast<f32x4v*>(dst) = f32x4v{v[0], v[1], v[2], v[3]};
+__device__ inline void store_v(E* dst, int have, const float* v) {
+    if constexpr (sizeof(E) == 2) {
+        Pack8<E> w;
+        w.round(v);
+        w.store(dst, have);
+    } else if (have >= V) {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) reinterpret_cast<AnyF*>(dst + h)->v = f32x4v{v[h], v[h + 1], v[h + 2], v[h + 3]};
     } else {
-        dst[0] = from_float<E>(v[0]);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e < have) dst[e] = v[e];
     }
 }
 
@@ -66,18 +87,18 @@ __device__ inline void row_sum(float (&v)[N], float* lds, int& turn) {
         for (int e = 0; e < N; ++e) v[e] += __shfl_xor(v[e], s, 64);
     if constexpr (TPR > 64) {
         constexpr int WAVES = TPR / 64;
-        static_assert(TPR == THREADS, "one row per workgroup");
-        float* const set = lds + turn * WAVES * N;
+        float* const set = lds + turn * (THREADS / 64) * N;
         turn ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int e = 0; e < N; ++e) set[(threadIdx.x >> 6) * N + e] = v[e];
         __syncthreads();
+        const float* const row = set + threadIdx.x / TPR * WAVES * N;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            float s = set[e];
+            float s = row[e];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) s += set[w * N + e];
+            for (int w = 1; w < WAVES; ++w) s += row[w * N + e];
             v[e] = s;
         }
     }
@@ -87,92 +108,82 @@ __device__ inline void row_sum(float (&v)[N], float* lds, int& turn) {
 template <class E, int V, int TPR, int THREADS, int ITEMS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormParams p) {
     constexpr int RPB = THREADS / TPR;
-    __shared__ float lds[TPR > 64 ? 2 * TPR / 64 : 1];
+    __shared__ float lds[TPR > 64 ? 2 * THREADS / 64 : 1];
     const int t = threadIdx.x % TPR;
     const float inv = 1.0f / (float)p.C;
     int turn = 0;
+    auto squares = [&](float* v, int have, float mean, float& sq) {  // v about the mean, and their squares
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = e < have ? v[e] - mean : 0.0f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) sq += v[e] * v[e];
+    };
+    auto finish = [&](float* v, E* y, int c, float rstd) {
+        const int have = p.C - c;
+        float g[V], b[V];
+        if (p.gamma) load_v<V>(p.gamma + c, have, g);
+        if (p.beta) load_v<V>(p.beta + c, have, b);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float o = v[e] * rstd;
+            if (p.gamma) o *= g[e];
+            if (p.beta) o += b[e];
+            v[e] = o;
+        }
+        store_v<V>(y + c, have, v);
+    };
     // every thread of a workgroup makes the same number of turns (the sums have barriers)
     for (int64_t first = (int64_t)blockIdx.x * RPB; first < p.rows; first += (int64_t)gridDim.x * RPB) {
         const int64_t row = first + threadIdx.x / TPR;
-        const bool have = row < p.rows;
-        const E* const x = static_cast<const E*>(p.X) + (have ? row : p.rows - 1) * p.ldx;
+        const bool here = row < p.rows;
+        const E* const x = static_cast<const E*>(p.X) + (here ? row : p.rows - 1) * p.ldx;
         E* const y = static_cast<E*>(p.Y) + row * p.ldy;
-        float sum[1] = {0.0f}, mean, rstd;
+        float sum[1] = {0.0f}, sq[1] = {0.0f}, mean, rstd;
         if constexpr (ITEMS > 0) {
             float v[ITEMS][V];
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
                 const int c = (i * TPR + t) * V;
-                if (c < p.C) load_v<V>(x + c, v[i]);
-                else
+                load_v<V>(x + c, p.C - c, v[i]);
+            }
 #pragma unroll
-                    for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+            for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[0] += v[i][e];
-            }
             row_sum<TPR, THREADS, 1>(sum, lds, turn);
             mean = sum[0] * inv;
-            float sq[1] = {0.0f};
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const bool in = (i * TPR + t) * V < p.C;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[i][e] -= mean;
-                    if (in) sq[0] += v[i][e] * v[i][e];
-                }
-            }
+            for (int i = 0; i < ITEMS; ++i) squares(v[i], p.C - (i * TPR + t) * V, mean, sq[0]);
             row_sum<TPR, THREADS, 1>(sq, lds, turn);
             rstd = 1.0f / sqrtf(sq[0] * inv + p.eps);
-            if (have)
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    const int c = (i * TPR + t) * V;
-                    if (c >= p.C) break;
-                    float g[V], b[V];
-                    if (p.gamma) load_v<V>(p.gamma + c, g);
-                    if (p.beta) load_v<V>(p.beta + c, b);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        float o = v[i][e] * rstd;
-                        if (p.gamma) o *= g[e];
-                        if (p.beta) o += b[e];
-                        v[i][e] = o;
-                    }
-                    store_v<V>(y + c, v[i]);
-                }
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = (i * TPR + t) * V;
+                if (here && c < p.C) finish(v[i], y, c, rstd);
+            }
         } else {
+            float v[V];
             for (int c = t * V; c < p.C; c += TPR * V) {
-                float v[V];
-                load_v<V>(x + c, v);
+                load_v<V>(x + c, p.C - c, v);
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[0] += v[e];
             }
             row_sum<TPR, THREADS, 1>(sum, lds, turn);
             mean = sum[0] * inv;
-            float sq[1] = {0.0f};
             for (int c = t * V; c < p.C; c += TPR * V) {
-                float v[V];
-                load_v<V>(x + c, v);
-#pragma unroll
-                for (int e = 0; e < V; ++e) sq[0] += (v[e] - mean) * (v[e] - mean);
+                load_v<V>(x + c, p.C - c, v);
+                squares(v, p.C - c, mean, sq[0]);
             }
             row_sum<TPR, THREADS, 1>(sq, lds, turn);
             rstd = 1.0f / sqrtf(sq[0] * inv + p.eps);
             for (int c = t * V; c < p.C; c += TPR * V) {
-                float v[V];
-                load_v<V>(x + c, v);
+                load_v<V>(x + c, p.C - c, v);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float o = (v[e] - mean) * rstd;
-                    if (p.gamma) o *= p.gamma[c + e];
-                    if (p.beta) o += p.beta[c + e];
-                    v[e] = o;
-                }
-                store_v<V>(y + c, v);
+                for (int e = 0; e < V; ++e) v[e] -= mean;
+                finish(v, y, c, rstd);
             }
         }
-        if (have && t == 0) {
+        if (here && t == 0) {
             if (p.mean) p.mean[row] = mean;
             if (p.rstd) p.rstd[row] = rstd;
         }
@@ -190,25 +201,24 @@ __device__ inline void join_columns(const float* v, float* lds, float* to, int c
         for (int e = 0; e < V; ++e) lds[threadIdx.x * V + e] = v[e];
         __syncthreads();
         if (threadIdx.x < TPR && c < C) {
+            float s[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                float s = v[e];
+                s[e] = v[e];
 #pragma unroll
-                for (int r = 1; r < RPB; ++r) s += lds[(r * TPR + threadIdx.x) * V + e];
-                to[c + e] = s;
+                for (int r = 1; r < RPB; ++r) s[e] += lds[(r * TPR + threadIdx.x) * V + e];
             }
+            store_v<V>(to + c, C - c, s);
         }
     } else {
-        if (c < C)
-#pragma unroll
-            for (int e = 0; e < V; ++e) to[c + e] = v[e];
+        if (c < C) store_v<V>(to + c, C - c, v);
     }
 }
 
 template <class E, int V, int TPR, int THREADS, int ITEMS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormParams p) {
     constexpr int RPB = THREADS / TPR;
-    constexpr int JOIN = RPB > 1 ? THREADS * V : 1, RED = TPR > 64 ? 4 * TPR / 64 : 1;
+    constexpr int JOIN = RPB > 1 ? THREADS * V : 1, RED = TPR > 64 ? 4 * THREADS / 64 : 1;
     __shared__ float lds[JOIN > RED ? JOIN : RED];
     const int t = threadIdx.x % TPR;
     const float inv = 1.0f / (float)p.C;
@@ -218,13 +228,15 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormParams p) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int c = (i * TPR + t) * V;
+        if (p.gamma) load_v<V>(p.gamma + c, p.C - c, gm[i]);
+        else
 #pragma unroll
-        for (int e = 0; e < V; ++e) gm[i][e] = p.gamma && c < p.C ? p.gamma[c + e] : 1.0f;
+            for (int e = 0; e < V; ++e) gm[i][e] = 1.0f;
     }
     for (int64_t first = (int64_t)blockIdx.x * RPB; first < p.rows; first += (int64_t)gridDim.x * RPB) {
         const int64_t at = first + threadIdx.x / TPR;
-        const bool have = at < p.rows;
-        const int64_t row = have ? at : p.rows - 1;
+        const bool here = at < p.rows;
+        const int64_t row = here ? at : p.rows - 1;
         const E* const x = static_cast<const E*>(p.X) + row * p.ldx;
         const E* const g = static_cast<const E*>(p.G) + row * p.ldg;
         const float mean = p.mean[row], rstd = p.rstd[row];
@@ -232,11 +244,11 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormParams p) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int c = (i * TPR + t) * V;
-            if (have && c < p.C) {
-                load_v<V>(x + c, xh[i]);
-                load_v<V>(g + c, w[i]);
+            if (here && c < p.C) {
+                load_v<V>(x + c, p.C - c, xh[i]);
+                load_v<V>(g + c, p.C - c, w[i]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
+                for (int e = 0; e < V; ++e) {  // (past the row's end g is 0)
                     xh[i][e] = (xh[i][e] - mean) * rstd;
                     dg[i][e] += w[i][e] * xh[i][e];
                     db[i][e] += w[i][e];
@@ -253,10 +265,10 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormParams p) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
                 const int c = (i * TPR + t) * V;
-                if (have && c < p.C) {
+                if (here && c < p.C) {
 #pragma unroll
                     for (int e = 0; e < V; ++e) w[i][e] = rstd * (w[i][e] - mw - xh[i][e] * mx);
-                    store_v<V>(y + c, w[i]);
+                    store_v<V>(y + c, p.C - c, w[i]);
                 }
             }
         }
@@ -271,7 +283,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormParams p) {
     }
 }
 
-// Rows longer than the registers hold: the partial sums of 256 columns (V = 1) ...
+// Rows longer than the registers hold: the partial sums of 256 columns ...
 template <class E>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormParams p, int64_t rows_per_share) {
     const int c = (int)(blockIdx.x * 256 + threadIdx.x);
@@ -314,7 +326,7 @@ __global__ __launch_bounds__(1024) void norm_long_grad_kernel(NormParams p) {
     }
 }
 
-constexpr int64_t kMaxBlocks = 16384;
+constexpr int64_t kMaxBlocks = int64_t(1) << 21;
 
 template <class E, int V, int TPR, int THREADS, int ITEMS>
 hipError_t forward(const NormParams& p, hipStream_t stream) {
@@ -324,22 +336,20 @@ hipError_t forward(const NormParams& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Threads per row: as few as hold it in at most 4 vectors (16 single elements) each, whole
-// waves from 64 on.
+// Threads per row: as few as hold it in at most 4 vectors each, whole waves from 64 on.
 template <class E, int V>
 hipError_t forward(const NormParams& p, hipStream_t stream) {
     const int64_t v = (p.C + V - 1) / V;
-    if constexpr (V > 1) {
-        if (v <= 16) return forward<E, V, 16, 256, 1>(p, stream);
-        if (v <= 64) return forward<E, V, 64, 256, 1>(p, stream);
-        if (v <= 256) return forward<E, V, 64, 256, 4>(p, stream);
-        if (v <= 1024) return forward<E, V, 256, 256, 4>(p, stream);
-        if (v <= 4096) return forward<E, V, 1024, 1024, 4>(p, stream);
-    } else {
-        if (v <= 64) return forward<E, V, 64, 256, 1>(p, stream);
-        if (v <= 512) return forward<E, V, 64, 256, 8>(p, stream);
-        if (v <= 4096) return forward<E, V, 256, 256, 16>(p, stream);
-    }
+    if (v <= 8) return forward<E, V, 8, 256, 1>(p, stream);
+    if (v <= 16) return forward<E, V, 16, 256, 1>(p, stream);
+    if (v <= 32) return forward<E, V, 32, 256, 1>(p, stream);
+    if (v <= 64) return forward<E, V, 64, 256, 1>(p, stream);
+    if (v <= 128) return forward<E, V, 64, 256, 2>(p, stream);
+    if (v <= 256) return forward<E, V, 128, 256, 2>(p, stream);
+    if (v <= 512) return forward<E, V, 256, 256, 2>(p, stream);
+    if (v <= 1024) return forward<E, V, 256, 256, 4>(p, stream);
+    if (v <= 2048) return forward<E, V, 512, 512, 4>(p, stream);
+    if (v <= 4096) return forward<E, V, 1024, 1024, 4>(p, stream);
     return forward<E, V, 1024, 1024, 0>(p, stream);
 }
 
@@ -352,17 +362,15 @@ hipError_t backward(const NormParams& p, uint32_t blocks, hipStream_t stream) {
 template <class E, int V>
 hipError_t backward(const NormParams& p, uint32_t blocks, hipStream_t stream) {
     const int64_t v = (p.C + V - 1) / V;
-    if constexpr (V > 1) {
-        if (v <= 16) return backward<E, V, 16, 256, 1>(p, blocks, stream);
-        if (v <= 64) return backward<E, V, 64, 256, 1>(p, blocks, stream);
-        if (v <= 128) return backward<E, V, 64, 256, 2>(p, blocks, stream);
-        if (v <= 512) return backward<E, V, 256, 256, 2>(p, blocks, stream);
-        if (v <= 2048) return backward<E, V, 1024, 1024, 2>(p, blocks, stream);
-    } else {
-        if (v <= 64) return backward<E, V, 64, 256, 1>(p, blocks, stream);
-        if (v <= 512) return backward<E, V, 64, 256, 8>(p, blocks, stream);
-        if (v <= 4096) return backward<E, V, 256, 256, 16>(p, blocks, stream);
-    }
+    if (v <= 8) return backward<E, V, 8, 256, 1>(p, blocks, stream);
+    if (v <= 16) return backward<E, V, 16, 256, 1>(p, blocks, stream);
+    if (v <= 32) return backward<E, V, 32, 256, 1>(p, blocks, stream);
+    if (v <= 64) return backward<E, V, 64, 256, 1>(p, blocks, stream);
+    if (v <= 128) return backward<E, V, 64, 256, 2>(p, blocks, stream);
+    if (v <= 256) return backward<E, V, 128, 256, 2>(p, blocks, stream);
+    if (v <= 512) return backward<E, V, 256, 256, 2>(p, blocks, stream);
+    if (v <= 1024) return backward<E, V, 512, 512, 2>(p, blocks, stream);
+    if (v <= 2048) return backward<E, V, 1024, 1024, 2>(p, blocks, stream);
     if (p.part) {
         const int64_t per = (p.rows + blocks - 1) / blocks;
         hipLaunchKernelGGL(norm_columns_kernel<E>, dim3((uint32_t)((p.C + 255) / 256), blocks), dim3(256), 0, stream, p, per);
@@ -371,11 +379,6 @@ hipError_t backward(const NormParams& p, uint32_t blocks, hipStream_t stream) {
         hipLaunchKernelGGL(norm_long_grad_kernel<E>, dim3((uint32_t)(p.rows < kMaxBlocks ? p.rows : kMaxBlocks)), dim3(1024), 0,
                            stream, p);
     return hipGetLastError();
-}
-
-bool vectors(const NormParams& p, int64_t width) {
-    return p.C % width == 0 && p.ldx % width == 0 && p.ldg % width == 0 && p.ldy % width == 0 &&
-           !(((uintptr_t)p.X | (uintptr_t)p.G | (uintptr_t)p.Y | (uintptr_t)p.gamma | (uintptr_t)p.beta) & 15u);
 }
 
 }  // namespace
@@ -394,15 +397,15 @@ hipError_t launch_norm(const void* X, int64_t ldx, const float* gamma, const flo
     p.ldy = ldy;
     p.C = C;
     p.eps = eps;
-    if (dtype) return vectors(p, 8) ? forward<uint16_t, 8>(p, stream) : forward<uint16_t, 1>(p, stream);
-    return vectors(p, 4) ? forward<float, 4>(p, stream) : forward<float, 1>(p, stream);
+    return dtype ? forward<uint16_t, 8>(p, stream) : forward<float, 4>(p, stream);
 }
 
-// Workgroups of the backward pass, each of which leaves 2 C partial sums: at most 1024, and
-// at least 16 rows each so that those stay a small part of the traffic.
+// Workgroups of the backward pass, each of which leaves 2 C partial sums: one per row up to
+// 256 (49 rows of 2048: one per 16 rows 20 us, so 9), then one per 16 rows, so that the
+// partial sums stay a small part of the traffic, up to 1024.
 int64_t norm_grad_blocks(int64_t rows) {
-    const int64_t b = (rows + 15) / 16;
-    return b < 1024 ? b : 1024;
+    const int64_t few = rows < 256 ? rows : 256, many = (rows + 15) / 16;
+    return many < few ? few : many < 1024 ? many : 1024;
 }
 
 hipError_t launch_norm_grad(const void* G, int64_t ldg, const void* X, int64_t ldx, const float* gamma, const float* mean,
@@ -422,9 +425,7 @@ hipError_t launch_norm_grad(const void* G, int64_t ldg, const void* X, int64_t l
     p.ldy = C;
     p.C = C;
     const uint32_t blocks = (uint32_t)norm_grad_blocks(rows);
-    hipError_t e;
-    if (dtype) e = vectors(p, 8) ? backward<uint16_t, 8>(p, blocks, stream) : backward<uint16_t, 1>(p, blocks, stream);
-    else e = vectors(p, 4) ? backward<float, 4>(p, blocks, stream) : backward<float, 1>(p, blocks, stream);
+    const hipError_t e = dtype ? backward<uint16_t, 8>(p, blocks, stream) : backward<float, 4>(p, blocks, stream);
     if (e != hipSuccess || !p.part) return e;
     return launch_sum_pairs(part, blocks, C, dgamma, dbeta, stream);
 }

@@ -176,13 +176,60 @@ __device__ inline u32x4v load_any(const uint16_t* src) {
     };
     return reinterpret_cast<const Any*>(src)->v;
 }
-__device__ inline u32x4v load_some(const uint16_t* src, int64_t have) {  // its first `have` elements, then zeros
+// its first `have` elements, then zeros: 8, 4 and 2 bytes, as `have` is made of
+__device__ inline u32x4v load_some(const uint16_t* src, int64_t have) {
     if (have >= 8) return load_any(src);
+    typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+    struct __attribute__((packed, aligned(2))) Any2 {
+        u32x2v v;
+    };
+    struct __attribute__((packed, aligned(2))) Any1 {
+        uint32_t v;
+    };
     u32x4v w = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < have) w[e / 2] |= (uint32_t)src[e] << (16 * (e % 2));
+    if (have <= 0) return w;
+    const int n = (int)have, two = n & 4, one = n & 6;
+    uint32_t pair = 0, last = 0;
+    if (n & 4) {
+        const u32x2v x = reinterpret_cast<const Any2*>(src)->v;
+        w[0] = x[0];
+        w[1] = x[1];
+    }
+    if (n & 2) pair = reinterpret_cast<const Any1*>(src + two)->v;
+    if (n & 1) last = src[one];
+    // pair goes to dword two / 2 (0 or 2), last to dword one / 2
+    if (n & 2) {
+        if (two) w[2] = pair;
+        else w[0] = pair;
+    }
+    if (n & 1) {
+        if (one == 0) w[0] = last;
+        else if (one == 2) w[1] = last;
+        else if (one == 4) w[2] = last;
+        else w[3] = last;
+    }
     return w;
+}
+// the first `have` of 8 elements to memory, likewise
+__device__ inline void store_some(uint16_t* dst, u32x4v w, int have) {
+    typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+    struct __attribute__((packed, aligned(2))) Any4 {
+        u32x4v v;
+    };
+    struct __attribute__((packed, aligned(2))) Any2 {
+        u32x2v v;
+    };
+    struct __attribute__((packed, aligned(2))) Any1 {
+        uint32_t v;
+    };
+    if (have >= 8) {
+        reinterpret_cast<Any4*>(dst)->v = w;
+    } else if (have > 0) {
+        const int two = have & 4, one = have & 6;
+        if (have & 4) reinterpret_cast<Any2*>(dst)->v = u32x2v{w[0], w[1]};
+        if (have & 2) reinterpret_cast<Any1*>(dst + two)->v = two ? w[2] : w[0];
+        if (have & 1) dst[one] = (uint16_t)(one == 0 ? w[0] : one == 2 ? w[1] : one == 4 ? w[2] : w[3]);
+    }
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -238,31 +285,28 @@ struct Pack8 {
     u32x4v w[W];
     // the first `have` of them
     __device__ inline void load(const E* src, int have) {
-        if (have >= 8) {
+        if constexpr (sizeof(E) == 2) {
+            w[0] = load_some(src, have);
+        } else if (have >= 8) {
 #pragma unroll
             for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const Any*>(src)[i].v;
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < have) set(e, src[e]);
+                if (e < have) w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, src[e]);
         }
     }
     __device__ inline void store(E* dst, int have) const {
-        if (have >= 8) {
+        if constexpr (sizeof(E) == 2) {
+            store_some(dst, w[0], have);
+        } else if (have >= 8) {
 #pragma unroll
             for (int i = 0; i < W; ++i) reinterpret_cast<Any*>(dst)[i].v = w[i];
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < have) {
-                    if constexpr (sizeof(E) == 4) dst[e] = __builtin_bit_cast(float, (uint32_t)w[e / 4][e % 4]);
-                    else dst[e] = (E)(w[0][e / 2] >> (16 * (e % 2)));
-                }
+                if (e < have) dst[e] = __builtin_bit_cast(float, (uint32_t)w[e / 4][e % 4]);
         }
-    }
-    __device__ inline void set(int e, E x) {
-        if constexpr (sizeof(E) == 4) w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, x);
-        else w[0][e / 2] = e % 2 ? (w[0][e / 2] & 0xffffu) | (uint32_t)x << 16 : (w[0][e / 2] & 0xffff0000u) | x;
     }
     __device__ inline float get(int e) const {
         if constexpr (sizeof(E) == 4) {
