@@ -406,11 +406,8 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     float* const part = static_cast<float*>(workspace);
     clear_stale_error();
     if (act != MEC_ACT_NONE || dbias) {
-        rc = hip_status(mec::launch_act_grad(G, g_pitch, Z, act == MEC_ACT_NONE ? nullptr : dZ, dbias ? part : nullptr, rows,
-                                             k_c, act, dtype, st), "gradient of the activation");
-        if (rc == MEC_OK && dbias)
-            rc = hip_status(mec::launch_sum_parts(part, mec::act_grad_shares(rows, k_c), k_c, dbias, MEC_F32, st),
-                            "gradient of the bias");
+        rc = hip_status(mec::launch_act_grad(G, g_pitch, Z, act == MEC_ACT_NONE ? nullptr : dZ, dbias, part, rows, k_c, act,
+                                             dtype, st), "gradients of the activation and the bias");
         if (rc != MEC_OK) return rc;
     }
     mec::Product p{};

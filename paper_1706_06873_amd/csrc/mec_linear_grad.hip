@@ -19,59 +19,68 @@ struct ActGradParams {
     int32_t N, act;
 };
 
-// V columns per thread, TX threads across the columns, 256 / TX rows at a time.
-template <class E, int V, int TX>
-__global__ __launch_bounds__(256) void act_grad_kernel(ActGradParams p) {
-    constexpr int TY = 256 / TX;
+// Strips of 8 TX columns, THREADS / TX rows at a time; rows at any boundary (Pack8).
+template <class E, int TX, int THREADS>
+__global__ __launch_bounds__(THREADS) void act_grad_kernel(ActGradParams p) {
+    constexpr int TY = THREADS / TX, U = 2;  // rows of a thread in flight
     constexpr bool FAST = sizeof(E) == 2;
-    __shared__ float sums[TY > 1 ? 256 * V : 1];
+    __shared__ __align__(16) float sums[THREADS * 8];
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
-    const int32_t n = (int32_t)(blockIdx.x * TX + tx) * V;
+    const int32_t n = (int32_t)(blockIdx.x * TX + tx) * 8, have = p.N - n;
     const int64_t r0 = (int64_t)blockIdx.y * p.rows_per_share;
     const int64_t r1 = r0 + p.rows_per_share < p.rows ? r0 + p.rows_per_share : p.rows;
-    float sum[V] = {};
-    if (n < p.N) {
-        for (int64_t r = r0 + ty; r < r1; r += TY) {
-            const E* const g = static_cast<const E*>(p.G) + r * p.ldg + n;
-            float x[V];
-            if constexpr (V == 8) load8v(g, x); else x[0] = to_float(g[0]);
-            if (p.act != kActNone) {
-                const E* const at = static_cast<const E*>(p.Z) + r * p.N + n;
-                float z[V];
-                if constexpr (V == 8) load8v(at, z); else z[0] = to_float(at[0]);
+    float sum[8] = {};
+    if (have > 0) {
+        for (int64_t r = r0 + ty; r < r1; r += U * TY) {
+            Pack8<E> g[U], z[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = r + u * TY < r1 ? r + u * TY : r;
+                g[u].load(static_cast<const E*>(p.G) + row * p.ldg + n, have);
+                if (p.act != kActNone) z[u].load(static_cast<const E*>(p.Z) + row * p.N + n, have);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (r + u * TY >= r1) break;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = g[u].get(e);
                 if (p.act == kActRelu) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] = z[e] > 0.0f ? x[e] : 0.0f;
+                    for (int e = 0; e < 8; ++e) x[e] = z[u].get(e) > 0.0f ? x[e] : 0.0f;
                 } else if (p.act == kActSilu) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] *= act_slope<FAST>(kActSilu, z[e]);
-                } else {
+                    for (int e = 0; e < 8; ++e) x[e] *= act_slope<FAST>(kActSilu, z[u].get(e));
+                } else if (p.act == kActGelu) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] *= act_slope<FAST>(kActGelu, z[e]);
+                    for (int e = 0; e < 8; ++e) x[e] *= act_slope<FAST>(kActGelu, z[u].get(e));
                 }
-            }
-            if (p.dZ) {
-                E* const to = static_cast<E*>(p.dZ) + r * p.N + n;
-                if constexpr (V == 8) store8v(to, x); else to[0] = from_float<E>(x[0]);
-            }
+                if (p.dZ) {
+                    Pack8<E> o;
+                    o.round(x);
+                    o.store(static_cast<E*>(p.dZ) + (r + u * TY) * p.N + n, have);
+                }
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += x[e];
+                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            }
         }
     }
     if (!p.part) return;  // (the same for every thread)
-    if constexpr (TY > 1) {
+    // joined in halves: row groups y and y + s
 #pragma unroll
-        for (int e = 0; e < V; ++e) sums[(ty * TX + tx) * V + e] = sum[e];
+    for (int e = 0; e < 8; ++e) sums[threadIdx.x * 8 + e] = sum[e];
+#pragma unroll
+    for (int s = TY / 2; s > 0; s >>= 1) {
         __syncthreads();
-        if (ty) return;
+        if (ty < s)
 #pragma unroll
-        for (int y = 1; y < TY; ++y)
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += sums[(y * TX + tx) * V + e];
+            for (int e = 0; e < 8; ++e) sums[threadIdx.x * 8 + e] = sum[e] += sums[(threadIdx.x + s * TX) * 8 + e];
     }
-    if (n < p.N)
-#pragma unroll
-        for (int e = 0; e < V; ++e) p.part[(int64_t)blockIdx.y * p.N + n + e] = sum[e];
+    if (ty == 0 && have > 0) {
+        Pack8<float> o;
+        o.round(sum);
+        o.store(p.part + (int64_t)blockIdx.y * p.N + n, have);
+    }
 }
 
 // Partial sums part[i*n + j], i < count: output j < n0 goes to out[j], the others to
@@ -133,20 +142,20 @@ hipError_t sum_parts(const float* part, int64_t count, int64_t n, int64_t n0, vo
     return hipGetLastError();
 }
 
-template <class E, int V, int TX>
+template <class E, int TX, int THREADS>
 hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
-    const uint32_t strips = (uint32_t)((p.N + V * TX - 1) / (V * TX));
-    hipLaunchKernelGGL((act_grad_kernel<E, V, TX>), dim3(strips, shares), dim3(256), 0, stream, p);
+    const uint32_t strips = (uint32_t)((p.N + 8 * TX - 1) / (8 * TX));
+    hipLaunchKernelGGL((act_grad_kernel<E, TX, THREADS>), dim3(strips, shares), dim3(THREADS), 0, stream, p);
     return hipGetLastError();
 }
 
+// Few rows (one share): 64 at a time, so that the column sums need no second launch. Else
+// strips of up to 1024 columns, as narrow as hold the row.
 template <class E>
 hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
-    constexpr int64_t W = 16 / sizeof(E);
-    const bool vec = p.N % 8 == 0 && p.ldg % W == 0 && !(((uintptr_t)p.G | (uintptr_t)p.Z | (uintptr_t)p.dZ) & 15u);
-    if (!vec) return p.N > 64 ? act_grad<E, 1, 256>(p, shares, stream) : act_grad<E, 1, 64>(p, shares, stream);
-    return p.N > 512 ? act_grad<E, 8, 128>(p, shares, stream)
-                     : p.N > 128 ? act_grad<E, 8, 32>(p, shares, stream) : act_grad<E, 8, 16>(p, shares, stream);
+    if (shares == 1) return act_grad<E, 16, 1024>(p, shares, stream);
+    return p.N > 512 ? act_grad<E, 128, 256>(p, shares, stream)
+                     : p.N > 128 ? act_grad<E, 32, 256>(p, shares, stream) : act_grad<E, 16, 256>(p, shares, stream);
 }
 
 }  // namespace
@@ -159,28 +168,31 @@ hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* 
     return sum_parts<float>(part, count, 2 * n, n, out, out2, stream);
 }
 
-// Shares of the rows: enough to fill the GPU, at least 32 rows each, and partial sums that
-// stay a small part of the traffic.
+// Shares of the rows: one up to 256 rows; else enough to fill the GPU, at least 32 rows each,
+// and partial sums that stay a small part of the traffic.
 int32_t act_grad_shares(int64_t rows, int64_t N) {
+    if (rows <= 256) return 1;
     const int64_t strips = (N + 511) / 512;
     int64_t shares = (rows + 31) / 32, most = 2048 / strips > 1 ? 2048 / strips : 1;
     return (int32_t)(shares < most ? shares : most);
 }
 
-hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* part, int64_t rows, int32_t N, int act,
-                           int dtype, hipStream_t stream) {
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* dbias, float* part, int64_t rows,
+                           int32_t N, int act, int dtype, hipStream_t stream) {
     const int32_t shares = act_grad_shares(rows, N);
     ActGradParams p{};
     p.G = G;
     p.Z = Z;
     p.dZ = dZ;
-    p.part = part;
+    p.part = !dbias ? nullptr : shares == 1 ? dbias : part;
     p.ldg = ldg;
     p.rows = rows;
     p.rows_per_share = (rows + shares - 1) / shares;
     p.N = N;
     p.act = act;
-    return dtype ? act_grad<uint16_t>(p, (uint32_t)shares, stream) : act_grad<float>(p, (uint32_t)shares, stream);
+    const hipError_t e = dtype ? act_grad<uint16_t>(p, (uint32_t)shares, stream) : act_grad<float>(p, (uint32_t)shares, stream);
+    if (e != hipSuccess || !dbias || shares == 1) return e;
+    return launch_sum_parts(part, shares, N, dbias, 0, stream);
 }
 
 }  // namespace mec

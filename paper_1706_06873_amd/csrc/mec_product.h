@@ -68,11 +68,11 @@ hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* o
 // the same for 2 n columns, the first n to out and the others to out2 (either may be nullptr)
 hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* out, float* out2, hipStream_t stream);
 
-// dZ = G act'(Z) (dZ nullptr: act is none and dZ is G) and, with part, the partial column
-// sums of dZ over act_grad_shares shares of the rows
+// dZ = G act'(Z) (dZ nullptr: act is none and dZ is G) and, unless nullptr, dbias, by way of
+// the partial column sums of act_grad_shares shares of the rows in part
 int32_t act_grad_shares(int64_t rows, int64_t N);
-hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* part, int64_t rows, int32_t N, int act,
-                           int dtype, hipStream_t stream);
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* dbias, float* part, int64_t rows,
+                           int32_t N, int act, int dtype, hipStream_t stream);
 
 // mec_norm.hip
 hipError_t launch_norm(const void* X, int64_t ldx, const float* gamma, const float* beta, void* Y, int64_t ldy, float* mean,
