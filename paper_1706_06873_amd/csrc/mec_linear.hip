@@ -69,9 +69,10 @@ struct Operand {
     int64_t step;       // bytes from chunk to chunk
     int64_t left;       // uniform: DMA, TR: bytes of rows from base on; else elements of the reduction from base on
     int64_t ld;         // elements
-    uint32_t voff[TR && DMA ? 1 : ITEMS];
-    int32_t have;       // TR: columns from this thread's on; else 8 k of this thread's granule start here
-    int32_t k_at;       // else: first k of this thread's granule
+    uint32_t voff[TR && DMA ? 1 : ITEMS];  // bytes from base
+    int32_t have;       // TR: columns from this thread's on
+    int32_t k_at;       // first k of this thread's granule(s)
+    bool inner;         // uniform; not DMA, TR: every column of the tile is there
 
     static __device__ inline int swizzle(int row) { return KT == 64 ? row & 7 : (row >> 1) & 3; }
 
@@ -91,8 +92,8 @@ struct Operand {
                 left = 2 * ((k1 - k0) * ld - r0);
             } else {
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) voff[i] = (uint32_t)(k + i * (THREADS * 8 / T));
-                k_at = col;
+                for (int i = 0; i < ITEMS; ++i) voff[i] = 2u * (uint32_t)((k + i * (THREADS * 8 / T)) * ld + col);
+                inner = r0 + T <= count;
                 left = k1 - k0;
             }
         } else {
@@ -105,7 +106,7 @@ struct Operand {
             for (int i = 0; i < ITEMS; ++i) {
                 int r = row + i * (THREADS / G);
                 if (r0 + r >= count) r = count - 1 - r0;  // rows past the last are not stored
-                voff[i] = DMA ? 2u * (uint32_t)(r * ld + 8 * kg) : (uint32_t)r;
+                voff[i] = 2u * (uint32_t)(r * ld + 8 * kg);
             }
         }
     }
@@ -130,13 +131,16 @@ struct Operand {
     }
     // else: this chunk to registers, and from there to LDS
     __device__ inline void load(u32x4v* r) const {
-        const uint16_t* const src = reinterpret_cast<const uint16_t*>(base);
+        auto at = [&](int i) { return reinterpret_cast<const uint16_t*>(base + voff[i]); };
+        if (left >= KT && (!TR || inner)) {  // (uniform)
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            if constexpr (TR)
-                r[i] = voff[i] < left ? load_some(src + voff[i] * ld + k_at, have) : u32x4v{0, 0, 0, 0};
-            else
-                r[i] = load_some(src + voff[i] * ld + k_at, left - k_at);
+            for (int i = 0; i < ITEMS; ++i) r[i] = load_any(at(i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                if constexpr (TR) r[i] = load_some(at(i), k_at + i * (THREADS * 8 / T) < left ? have : 0);
+                else r[i] = load_some(at(i), left - k_at);
+            }
         }
     }
     static __device__ inline void put(const u32x4v* r, char* to, int tid) {
