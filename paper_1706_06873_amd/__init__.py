@@ -474,26 +474,45 @@ def conv2d_wgrad_noalloc(I, G, k_h, k_w, s_h=1, s_w=1, dK=None, stream=None):
 # are float32 or bfloat16, all the same; bias, gamma, beta, their gradients and the row
 # statistics are float32.
 
-def _rows(t, name, width=None, dtype=None, ref=None):
-    """(rows, channels, pitch) of an activation."""
-    if t.dim() < 2:
-        raise ValueError("%s must have the channels as its last dimension and at least one more" % name)
-    c = t.shape[-1]
-    if width is not None and c != width:
-        raise ValueError("%s must have %d channels, got %d" % (name, width, c))
-    if dtype is not None and t.dtype != dtype:
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_F32 = torch.float32
+# the current stream's handle without a Stream object around it (1.8 us of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = torch.cuda.current_device
+
+
+def _activations(t, name, c, dtype, device):
+    """The row pitch of activations of c channels."""
+    if t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if ref is not None:
-        _same_device(t, ref, name)
+    if t.device != device:
+        raise ValueError("%s is on %s, the inputs on %s" % (name, t.device, device))
+    return _pitch(t, name, c)
+
+
+def _pitch(t, name, c):
     if t.is_contiguous():
-        return (t.numel() // c if c else 0), c, c
+        return c
     if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= c:
-        return t.shape[0], c, t.stride(0)
+        return t.stride(0)
     raise ValueError("%s must be contiguous, or rows of contiguous channels" % name)
 
 
+def _channels(t, name):
+    """(shape, rows, channels) of activations, and their dtype's code."""
+    shape = t.shape
+    if len(shape) < 2:
+        raise ValueError("%s must have the channels as its last dimension and at least one more" % name)
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    c = shape[-1]
+    return shape, (t.numel() // c if c else 0), c, dt
+
+
 def _ptr(t, name):
-    """The device pointer of an activation that _rows has checked, or None."""
+    """The device pointer of a checked tensor, or None."""
     if t is None:
         return None
     if not t.is_cuda:
@@ -501,54 +520,81 @@ def _ptr(t, name):
     return t.data_ptr()
 
 
-def _param(t, n, name, ref):
-    """The pointer of a float32 parameter vector of n elements, or None."""
-    if t is None:
-        return None
-    if tuple(t.shape) != (n,) or t.dtype != torch.float32:
-        raise ValueError("%s must be torch.float32 of shape %s, got %s of shape %s"
-                         % (name, (n,), t.dtype, tuple(t.shape)))
-    _same_device(t, ref, name)
-    return _dev_ptr(t, name)
+def _dense(t, shape, dtype, device, name):
+    """Checks a dense tensor of exactly this shape, dtype and device."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError("%s must be %s of shape %s, got %s of shape %s"
+                         % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on %s, the inputs on %s" % (name, t.device, device))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
 
 
 def _new(t, shape, dtype, ref, name):
     """A given dense output, checked, or a new one."""
     if t is None:
         return ref.new_empty(shape, dtype=dtype)
-    _check_out(t, shape, dtype, ref, name)
+    _dense(t, shape, dtype, ref.device, name)
     return t
 
 
 def _act_code(act):
-    if act not in _ACTS:
+    code = _ACTS.get(act)
+    if code is None:
         raise ValueError("act must be one of %s, got %r" % (", ".join(sorted(_ACTS)), act))
-    return _ACTS[act]
+    return code
 
 
-# the current stream's handle without a Stream object around it (1.8 us of a call)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
-def _launch(name, ref, stream, *args):
-    """Calls an entry point on ref's device: the stream is its last argument."""
-    index = ref.device.index
-    if index != torch.cuda.current_device():
+def _launch(name, device, *args):
+    """Calls an entry point on that device's current stream, its last argument."""
+    index = device.index
+    if index != _current_device():
         with torch.cuda.device(index):
-            return _launch(name, ref, stream, *args)
-    status = getattr(lib, name)(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+            return _launch(name, device, *args)
+    status = getattr(lib, name)(*args, _raw_stream(index))
     if status < 0:
         raise MecError(status, name)
 
 
-def _matrix(K, name="K"):
+def _on(stream, call, ref, *args, **kwargs):
+    """The call with `stream` as the current stream, so that what it allocates (outputs,
+    workspaces) belongs to that stream too: memory that the caller's stream still uses, or
+    uses again once a workspace is dropped, is not handed to it."""
+    if stream.device != ref.device:
+        raise ValueError("stream is on %s, the inputs on %s" % (stream.device, ref.device))
+    with torch.cuda.stream(stream):
+        return call(ref, *args, **kwargs)
+
+
+def _scratch(need, workspace, ref):
+    """(workspace, bytes): a given one is checked for size and device, else one is made."""
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=ref.device), need
+    nbytes = workspace.numel() * workspace.element_size()
+    if workspace.device != ref.device:
+        raise ValueError("workspace is on %s, the inputs on %s" % (workspace.device, ref.device))
+    if nbytes < need:
+        raise ValueError("the workspace holds %d bytes, %d are needed" % (nbytes, need))
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace, nbytes
+
+
+def _matrix(K, dtype, device):
     """(i_c, k_c) of a kernel that acts on pixels: i_c x k_c, or 1 x 1 x i_c x k_c."""
-    if K.dim() == 4 and K.shape[0] == K.shape[1] == 1:
-        return K.shape[2], K.shape[3]
-    if K.dim() != 2:
-        raise ValueError("%s must be i_c x k_c, or 1 x 1 x i_c x k_c" % name)
-    return K.shape[0], K.shape[1]
+    shape = K.shape
+    if len(shape) == 4 and shape[0] == shape[1] == 1:
+        shape = shape[2:]
+    elif len(shape) != 2:
+        raise ValueError("K must be i_c x k_c, or 1 x 1 x i_c x k_c")
+    if K.dtype != dtype:
+        raise TypeError("K and the activations must have the same dtype")
+    if K.device != device:
+        raise ValueError("K is on %s, the inputs on %s" % (K.device, device))
+    if not K.is_contiguous():
+        raise ValueError("K must be contiguous")
+    return shape
 
 
 def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=None, Z=None, stream=None):
@@ -556,27 +602,35 @@ def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=N
     every pixel of X (... x i_c) and K of i_c x k_c (or 1 x 1 x i_c x k_c); act is "none",
     "relu", "silu" or "gelu" (the tanh form). A given Z (Y's shape) receives act's argument,
     for linear_grad. residual may be Y itself. Returns Y."""
-    i_c, k_c = _matrix(K)
-    dt = _dtype_code(X)
-    rows, _, x_pitch = _rows(X, "X", i_c)
-    if K.dtype != X.dtype:
-        raise TypeError("X and K must have the same dtype")
-    _same_device(K, X, "K")
+    if stream is not None:
+        return _on(stream, linear, X, K, bias, residual, act, residual_first, Y, Z)
+    xs, rows, i_c, dt = _channels(X, "X")
+    device, dtype = X.device, X.dtype
+    ki, k_c = _matrix(K, dtype, device)
+    if ki != i_c:
+        raise ValueError("X must have %d channels, got %d" % (ki, i_c))
+    x_pitch = _pitch(X, "X", i_c)
     a = _act_code(act)
-    shape = tuple(X.shape[:-1]) + (k_c,)
+    shape = xs[:-1] + (k_c,)
     r_pitch = 0
+    if bias is not None:
+        _dense(bias, (k_c,), _F32, device, "bias")
     if residual is not None:
-        if tuple(residual.shape) != shape:
-            raise ValueError("residual must be of shape %s, got %s" % (shape, tuple(residual.shape)))
-        r_pitch = _rows(residual, "residual", k_c, X.dtype, X)[2]
-    Y = _new(Y, shape, X.dtype, X, "Y")
-    y_pitch = _rows(Y, "Y")[2]
+        if residual.shape != shape:
+            raise ValueError("residual must be of shape %s, got %s" % (tuple(shape), tuple(residual.shape)))
+        r_pitch = _activations(residual, "residual", k_c, dtype, device)
+    y_pitch = k_c
+    if Y is None:
+        Y = X.new_empty(shape)
+    else:
+        if Y.shape != shape or Y.dtype != dtype:
+            raise ValueError("Y must be %s of shape %s, got %s of shape %s"
+                             % (dtype, tuple(shape), Y.dtype, tuple(Y.shape)))
+        y_pitch = _activations(Y, "Y", k_c, dtype, device)
     if Z is not None:
-        _check_out(Z, shape, X.dtype, X, "Z")
-    bias = _param(bias, k_c, "bias", X)
-    _launch("mec_linear", X, stream, _ptr(X, "X"), _dev_ptr(K, "K"), bias,
-            _ptr(residual, "residual"), _ptr(Y, "Y"), None if Z is None else _dev_ptr(Z, "Z"), rows, i_c, k_c,
-            x_pitch, r_pitch, y_pitch, dt, a, int(bool(residual_first)))
+        _dense(Z, shape, dtype, device, "Z")
+    _launch("mec_linear", device, _ptr(X, "X"), _ptr(K, "K"), _ptr(bias, "bias"), _ptr(residual, "residual"),
+            _ptr(Y, "Y"), _ptr(Z, "Z"), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0)
     return Y
 
 
@@ -592,56 +646,66 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     itself with act "none"; the residual's gradient is dZ where it was added first, else G.
     dK has K's dtype and shape, dbias is float32. A given workspace holds at least
     linear_grad_workspace_bytes bytes."""
-    i_c, k_c = _matrix(K)
-    dt = _dtype_code(G)
-    rows, _, g_pitch = _rows(G, "G", k_c)
-    if K.dtype != G.dtype:
-        raise TypeError("G and K must have the same dtype")
-    _same_device(K, G, "K")
+    if stream is not None:
+        return _on(stream, linear_grad, G, X, K, Z, act, needs, dZ, dX, dK, dbias, workspace)
+    gs, rows, k_c, dt = _channels(G, "G")
+    device, dtype = G.device, G.dtype
+    i_c, kc = _matrix(K, dtype, device)
+    if kc != k_c:
+        raise ValueError("G must have %d channels, got %d" % (kc, k_c))
+    g_pitch = _pitch(G, "G", k_c)
     a = _act_code(act)
     need_x, need_k, need_b = needs
-    x_pitch = i_c
+    x_pitch, shape = i_c, gs[:-1] + (i_c,)
     if X is not None:
-        if tuple(X.shape[:-1]) != tuple(G.shape[:-1]):
-            raise ValueError("X and G must have the same pixels, got %s and %s" % (tuple(X.shape), tuple(G.shape)))
-        x_pitch = _rows(X, "X", i_c, G.dtype, G)[2]
+        if X.shape != shape:
+            raise ValueError("X must be of shape %s, got %s" % (tuple(shape), tuple(X.shape)))
+        x_pitch = _activations(X, "X", i_c, dtype, device)
     elif need_k:
         raise ValueError("X is needed for dK")
     if a:
         if Z is None:
             raise ValueError("Z is needed with act %r" % act)
-        if tuple(Z.shape) != tuple(G.shape) or Z.dtype != G.dtype:
-            raise ValueError("Z must be %s of shape %s, got %s of shape %s"
-                             % (G.dtype, tuple(G.shape), Z.dtype, tuple(Z.shape)))
-        _same_device(Z, G, "Z")
-        dZ = _new(dZ, tuple(G.shape), G.dtype, G, "dZ")
-    dX = _new(dX, tuple(G.shape[:-1]) + (i_c,), G.dtype, G, "dX") if need_x else None
-    dK = _new(dK, tuple(K.shape), G.dtype, G, "dK") if need_k else None
-    dbias = _new(dbias, (k_c,), torch.float32, G, "dbias") if need_b else None
-    wp, wb = None, 0
+        _dense(Z, gs, dtype, device, "Z")
+        dZ = _new(dZ, gs, dtype, G, "dZ")
+    else:
+        Z, dZ = None, G
+    dX = _new(dX, shape, dtype, G, "dX") if need_x else None
+    dK = _new(dK, K.shape, dtype, G, "dK") if need_k else None
+    dbias = _new(dbias, (k_c,), _F32, G, "dbias") if need_b else None
+    nbytes = 0
     if need_k or need_b:
-        need = linear_grad_workspace_bytes(rows, i_c, k_c, dt)
-        workspace, wp, wb = _given_workspace(need, workspace, G)
-    opt = lambda t, name: None if t is None else _dev_ptr(t, name)  # noqa: E731
-    _launch("mec_linear_grad", G, stream, _ptr(G, "G"), _ptr(X, "X"), _dev_ptr(K, "K"),
-            opt(Z, "Z") if a else None, opt(dZ, "dZ") if a else None, opt(dX, "dX"), opt(dK, "dK"),
-            opt(dbias, "dbias"), wp, wb, rows, i_c, k_c, g_pitch, x_pitch, dt, a)
-    return dX, dK, dbias, dZ if a else G
+        workspace, nbytes = _scratch(linear_grad_workspace_bytes(rows, i_c, k_c, dt), workspace, G)
+    _launch("mec_linear_grad", device, _ptr(G, "G"), _ptr(X, "X"), _ptr(K, "K"), _ptr(Z, "Z"),
+            _ptr(dZ, "dZ") if a else None, _ptr(dX, "dX"), _ptr(dK, "dK"), _ptr(dbias, "dbias"),
+            _ptr(workspace, "workspace") if nbytes else None, nbytes, rows, i_c, k_c, g_pitch, x_pitch, dt, a)
+    return dX, dK, dbias, dZ
 
 
 def layer_norm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
     """Layer norm of every pixel's channels, (X - mean) rstd gamma + beta with rstd =
     1 / sqrt(variance + eps). Returns (Y, mean, rstd); mean and rstd (X's shape without the
     channels, float32) are what layer_norm_grad takes. Y may be X itself."""
-    dt = _dtype_code(X)
-    rows, c, x_pitch = _rows(X, "X")
-    Y = _new(Y, tuple(X.shape), X.dtype, X, "Y")
-    y_pitch = _rows(Y, "Y")[2]
-    mean = _new(mean, tuple(X.shape[:-1]), torch.float32, X, "mean")
-    rstd = _new(rstd, tuple(X.shape[:-1]), torch.float32, X, "rstd")
-    gamma, beta = _param(gamma, c, "gamma", X), _param(beta, c, "beta", X)
-    _launch("mec_layer_norm", X, stream, _ptr(X, "X"), gamma, beta,
-            _ptr(Y, "Y"), _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), rows, c, x_pitch, y_pitch, eps, dt)
+    if stream is not None:
+        return _on(stream, layer_norm, X, gamma, beta, eps, Y, mean, rstd)
+    shape, rows, c, dt = _channels(X, "X")
+    device, pixels = X.device, shape[:-1]
+    x_pitch = y_pitch = _pitch(X, "X", c)
+    if gamma is not None:
+        _dense(gamma, (c,), _F32, device, "gamma")
+    if beta is not None:
+        _dense(beta, (c,), _F32, device, "beta")
+    if Y is None:
+        Y, y_pitch = X.new_empty(shape), c
+    elif Y is not X:
+        if Y.shape != shape or Y.dtype != X.dtype:
+            raise ValueError("Y must be %s of shape %s, got %s of shape %s"
+                             % (X.dtype, tuple(shape), Y.dtype, tuple(Y.shape)))
+        y_pitch = _activations(Y, "Y", c, X.dtype, device)
+    mean = _new(mean, pixels, _F32, X, "mean")
+    rstd = _new(rstd, pixels, _F32, X, "rstd")
+    _launch("mec_layer_norm", device, _ptr(X, "X"), _ptr(gamma, "gamma"), _ptr(beta, "beta"), _ptr(Y, "Y"),
+            _ptr(mean, "mean"), _ptr(rstd, "rstd"), rows, c, x_pitch, y_pitch, eps, dt)
     return Y, mean, rstd
 
 
@@ -655,25 +719,27 @@ def layer_norm_grad(G, X, mean, rstd, gamma=None, needs=(True, True, True), dX=N
     """Gradients of layer_norm for G = dloss/dY: (dX, dgamma, dbeta), of which `needs` says
     which are wanted; the others come back as None. A given workspace holds at least
     layer_norm_grad_workspace_bytes bytes."""
-    dt = _dtype_code(X)
-    rows, c, x_pitch = _rows(X, "X")
-    if tuple(G.shape) != tuple(X.shape):
-        raise ValueError("G must be of shape %s, got %s" % (tuple(X.shape), tuple(G.shape)))
-    g_pitch = _rows(G, "G", c, X.dtype, X)[2]
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        _check_out(t, tuple(X.shape[:-1]), torch.float32, X, name)
+    if stream is not None:
+        return _on(stream, layer_norm_grad, G, X, mean, rstd, gamma, needs, dX, dgamma, dbeta, workspace)
+    shape, rows, c, dt = _channels(X, "X")
+    device, dtype, pixels = X.device, X.dtype, shape[:-1]
+    x_pitch = _pitch(X, "X", c)
+    if G.shape != shape:
+        raise ValueError("G must be of shape %s, got %s" % (tuple(shape), tuple(G.shape)))
+    g_pitch = _activations(G, "G", c, dtype, device)
+    _dense(mean, pixels, _F32, device, "mean")
+    _dense(rstd, pixels, _F32, device, "rstd")
     if gamma is not None:
-        _check_out(gamma, (c,), torch.float32, X, "gamma")
-    dX = _new(dX, tuple(X.shape), X.dtype, X, "dX") if needs[0] else None
-    dgamma = _new(dgamma, (c,), torch.float32, X, "dgamma") if needs[1] else None
-    dbeta = _new(dbeta, (c,), torch.float32, X, "dbeta") if needs[2] else None
-    wp, wb = None, 0
+        _dense(gamma, (c,), _F32, device, "gamma")
+    dX = _new(dX, shape, dtype, X, "dX") if needs[0] else None
+    dgamma = _new(dgamma, (c,), _F32, X, "dgamma") if needs[1] else None
+    dbeta = _new(dbeta, (c,), _F32, X, "dbeta") if needs[2] else None
+    nbytes = 0
     if needs[1] or needs[2]:
-        workspace, wp, wb = _given_workspace(layer_norm_grad_workspace_bytes(rows, c, dt), workspace, X)
-    opt = lambda t, name: None if t is None else _dev_ptr(t, name)  # noqa: E731
-    _launch("mec_layer_norm_grad", X, stream, _ptr(G, "G"), _ptr(X, "X"), opt(gamma, "gamma"),
-            _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), opt(dX, "dX"), opt(dgamma, "dgamma"),
-            opt(dbeta, "dbeta"), wp, wb, rows, c, g_pitch, x_pitch, dt)
+        workspace, nbytes = _scratch(layer_norm_grad_workspace_bytes(rows, c, dt), workspace, X)
+    _launch("mec_layer_norm_grad", device, _ptr(G, "G"), _ptr(X, "X"), _ptr(gamma, "gamma"), _ptr(mean, "mean"),
+            _ptr(rstd, "rstd"), _ptr(dX, "dX"), _ptr(dgamma, "dgamma"), _ptr(dbeta, "dbeta"),
+            _ptr(workspace, "workspace") if nbytes else None, nbytes, rows, c, g_pitch, x_pitch, dt)
     return dX, dgamma, dbeta
 
 
@@ -688,15 +754,23 @@ def orthogonalize(U, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
     (k_h x k_w x i_c x k_c, taken as the (k_h*k_w*i_c) x k_c matrix) or a stack of those.
     X = U / (|U|_F + eps), then X <- a X + (b A + c A^2) X with A = X X^T, `steps` times.
     Returns O of U's shape; it may be U itself."""
-    dt = _dtype_code(U)
-    if U.dim() not in (2, 3, 4, 5):
+    if stream is not None:
+        return _on(stream, orthogonalize, U, steps, coefficients, eps, O, workspace)
+    shape = U.shape
+    if len(shape) not in (2, 3, 4, 5):
         raise ValueError("U must be a matrix, a kernel's gradient or a stack of either")
-    batch = U.shape[0] if U.dim() % 2 else 1
-    cols = U.shape[-1]
+    dt = _DTYPES.get(U.dtype)
+    if dt is None:
+        raise TypeError("U must be float32 or bfloat16, got %s" % U.dtype)
+    if not U.is_contiguous():
+        raise ValueError("U must be contiguous")
+    batch = shape[0] if len(shape) % 2 else 1
+    cols = shape[-1]
     rows = U.numel() // (batch * cols) if batch * cols else 0
     a, b, c = coefficients
-    O = _new(O, tuple(U.shape), U.dtype, U, "O")
-    workspace, wp, wb = _given_workspace(orthogonalize_workspace_bytes(batch, rows, cols, dt), workspace, U)
-    _launch("mec_orthogonalize", U, stream, _dev_ptr(U, "U"), _dev_ptr(O, "O"), wp, wb, batch, rows, cols, steps,
-            a, b, c, eps, dt)
+    need = orthogonalize_workspace_bytes(batch, rows, cols, dt)
+    O = _new(O, shape, U.dtype, U, "O")
+    workspace, nbytes = _scratch(need, workspace, U)
+    _launch("mec_orthogonalize", U.device, _ptr(U, "U"), _ptr(O, "O"), _ptr(workspace, "workspace"), nbytes,
+            batch, rows, cols, steps, a, b, c, eps, dt)
     return O

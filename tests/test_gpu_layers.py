@@ -479,3 +479,23 @@ def test_streams_and_repeatability():
     for o in outs:
         for a, b in zip(want, o):
             assert torch.equal(a, b)
+
+
+def test_a_given_stream_owns_what_the_call_allocates():
+    """Workspaces and outputs made inside a call on another stream are not memory that the
+    caller's stream hands out again meanwhile."""
+    g = torch.Generator().manual_seed(22)
+    X, K = randn(g, 20000, 128).to(DEV), randn(g, 128, 256).to(DEV)
+    G, U = randn(g, 20000, 256).to(DEV), randn(g, 4, 600, 128).to(DEV)
+    want = mec.linear_grad(G, X, K)[:3] + (mec.orthogonalize(U), mec.linear(X, K)) + mec.layer_norm(X)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = mec.linear_grad(G, X, K, stream=side)[:3] + (mec.orthogonalize(U, stream=side), mec.linear(X, K, stream=side))
+        got += mec.layer_norm(X, stream=side)
+        busy = [torch.full((1 << 20,), 3.0, device=DEV) for _ in range(40)]  # the caller's stream goes on
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+        del busy

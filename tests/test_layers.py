@@ -119,6 +119,7 @@ def test_binding_refuses_linear_operands():
     for kw, error, match in [
         (dict(X=_t(2, 3, 4)), ValueError, "channels"), (dict(X=_t(5)), ValueError, "channels"),
         (dict(X=X.double()), TypeError, "float32 or bfloat16"), (dict(X=X.bfloat16()), TypeError, "same dtype"),
+        (dict(K=_t(6, 5).t()), ValueError, "K must be contiguous"), (dict(K=_t(4, 6)), ValueError, "X must have"),
         (dict(K=_t(5)), ValueError, "K must be"), (dict(K=_t(3, 1, 5, 6)), ValueError, "K must be"),
         (dict(X=X.permute(1, 0, 2, 3)), ValueError, "contiguous"), (dict(X=_t(1, 5).expand(7, 5)), ValueError, "contiguous"),
         (dict(X=_t(7, 10)[:, ::2]), ValueError, "contiguous"),
@@ -136,8 +137,8 @@ def test_binding_refuses_linear_operands():
 def test_binding_refuses_linear_gradients():
     G, X, K, Z = _t(8, 6), _t(8, 5), _t(5, 6), _t(8, 6)
     for kw, error, match in [
-        (dict(G=_t(8, 5)), ValueError, "G must have"), (dict(X=_t(7, 5)), ValueError, "same pixels"),
-        (dict(X=_t(8, 6)), ValueError, "X must have"), (dict(X=X.bfloat16()), TypeError, "X must be"),
+        (dict(G=_t(8, 5)), ValueError, "G must have"), (dict(X=_t(7, 5)), ValueError, "X must be of shape"),
+        (dict(X=_t(8, 6)), ValueError, "X must be of shape"), (dict(X=X.bfloat16()), TypeError, "X must be"),
         (dict(K=K.bfloat16()), TypeError, "same dtype"), (dict(X=None), ValueError, "X is needed"),
         (dict(act="relu"), ValueError, "Z is needed"), (dict(act="relu", Z=_t(8, 5)), ValueError, "Z must be"),
         (dict(act="relu", Z=Z.bfloat16()), ValueError, "Z must be"),
