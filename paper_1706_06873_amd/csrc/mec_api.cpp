@@ -342,7 +342,7 @@ int first_error(std::initializer_list<int> codes) {
 bool valid_act(int act) { return act >= MEC_ACT_NONE && act <= MEC_ACT_GELU; }
 
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
-    const int64_t s = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, true).splits;
+    const int64_t s = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, 64).splits;
     const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = mec::act_grad_shares(rows, k_c) * k_c * 4;
     return dk > db ? dk : db;
 }
@@ -439,7 +439,7 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
         p.N = k_c;
         p.K = (int32_t)rows;
         p.part = part;
-        const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, true);
+        const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, 64);
         rc = hip_status(mec::launch_product(plan, mec::Layout::kXtK, p, dtype, st), "gradient of the kernel");
         if (rc == MEC_OK && plan.splits > 1)
             rc = hip_status(mec::launch_sum_parts(part, plan.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
@@ -579,7 +579,7 @@ int mec_internal_wgrad(int kernel, const void* A, const float* G, float* dK, voi
 }
 
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
-    const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split != 0);
+    const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? 64 : 1);
     return p.kernel + 16 * p.splits;
 }
 

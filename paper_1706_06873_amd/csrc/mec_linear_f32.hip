@@ -125,12 +125,15 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
     __shared__ uint32_t lost_s;  // some thread's split left bits out
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % C::kWM, wn = wave / C::kWM;
-    const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
+    constexpr bool SQUARE = C::TM == C::TN && BM * BN == 1;  // holds symmetric products
+    const bool symmetric = SQUARE && p.symmetric;
+    const uint32_t tiles = symmetric ? (uint32_t)p.m_tiles * ((uint32_t)p.m_tiles + 1) / 2 : (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
-    const uint32_t share = b / tiles;  // of the reduction, or which product of a batch
-    const int32_t split = p.splits > 1 ? (int32_t)share : 0, bat = p.splits > 1 ? 0 : (int32_t)share;
+    const uint32_t share = b / tiles;  // of the reduction, for each product of a batch
+    const int32_t split = (int32_t)(share / (uint32_t)p.batch), bat = (int32_t)(share - (uint32_t)split * (uint32_t)p.batch);
     uint32_t mt, nt;
-    tile_of(b - share * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
+    if (symmetric) tile_of_half(b - share * tiles, mt, nt);
+    else tile_of(b - share * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
     const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
     const int64_t k0 = (int64_t)split * p.chunks * kKT;
     const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
@@ -239,6 +242,9 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
                 acc[i][j] = plain_block(A + m * ars + k0 * aks, aks, B + n * brs + k0 * bks, bks, (int32_t)(k1 - k0), lane);
             }
     }
+    if constexpr (SQUARE) {
+        if (symmetric && mt != nt) mirror(p, acc[0][0], mw, nw, bat, split, lane);
+    }
     epilogue<float, BM, BN>(p, acc, mine, mw, nw, bat, split, lane);
 }
 
@@ -250,7 +256,8 @@ hipError_t run(Product p, hipStream_t stream) {
     // shares are whole multiples of 64 elements, as product_splits counts them
     const int64_t chunks = 2 * (((int64_t)p.K + 63) / 64);
     p.chunks = 2 * (int32_t)((chunks / 2 + p.splits - 1) / p.splits);
-    const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * (p.splits > 1 ? p.splits : p.batch);
+    const int64_t tiles = p.symmetric ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles;
+    const int64_t blocks = tiles * p.splits * p.batch;
     if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
     if constexpr (L != Layout::kXtK) {
         if (p.K % 8) {

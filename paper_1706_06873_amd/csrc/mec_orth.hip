@@ -20,7 +20,7 @@
 namespace mec {
 namespace {
 
-constexpr int kShares = 64;  // of a matrix, for its norm
+constexpr int kShares = 128;  // of a matrix, for its norm
 
 struct OrthParams {
     const void* U;
@@ -36,10 +36,14 @@ template <class E, int THREADS>
 __device__ inline double sum_squares(const E* u, int64_t from, int64_t end) {
     __shared__ double sums[THREADS / 64];
     double s = 0.0;
-#pragma unroll 4
-    for (int64_t i = from + threadIdx.x; i < end; i += THREADS) {
-        const double x = (double)to_float(u[i]);
-        s += x * x;
+#pragma unroll 2
+    for (int64_t i = from + threadIdx.x * 8; i < end; i += THREADS * 8) {
+        Pack8<E> w;
+        const int have = end - i < 8 ? (int)(end - i) : 8;
+        w.load(u + i, have);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < have) s += (double)w.get(e) * (double)w.get(e);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
@@ -49,6 +53,23 @@ __device__ inline double sum_squares(const E* u, int64_t from, int64_t end) {
 #pragma unroll
     for (int w = 1; w < THREADS / 64; ++w) s += sums[w];
     return s;
+}
+
+// x = by u
+template <class E, int THREADS>
+__device__ inline void scaled(const E* u, float* x, int64_t from, int64_t end, double by) {
+#pragma unroll 2
+    for (int64_t i = from + threadIdx.x * 8; i < end; i += THREADS * 8) {
+        Pack8<E> w;
+        const int have = end - i < 8 ? (int)(end - i) : 8;
+        w.load(u + i, have);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)((double)w.get(e) * by);
+        Pack8<float> o;
+        o.round(v);
+        o.store(x + i, have);
+    }
 }
 
 template <class E>
@@ -62,13 +83,11 @@ __global__ __launch_bounds__(256) void norm_squares_kernel(OrthParams p) {
 template <class E>
 __global__ __launch_bounds__(256) void scale_kernel(OrthParams p) {
     double s = 0.0;
+#pragma unroll 16
     for (int i = 0; i < kShares; ++i) s += p.part[blockIdx.y * kShares + i];
-    const double by = 1.0 / (sqrt(s) + (double)p.eps);
-    const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.y * p.n;
-    float* const x = p.X + (int64_t)blockIdx.y * p.n;
     const int64_t end = (blockIdx.x + 1) * p.per < p.n ? (blockIdx.x + 1) * p.per : p.n;
-#pragma unroll 4
-    for (int64_t i = blockIdx.x * p.per + threadIdx.x; i < end; i += 256) x[i] = (float)((double)to_float(u[i]) * by);
+    scaled<E, 256>(static_cast<const E*>(p.U) + blockIdx.y * p.n, p.X + blockIdx.y * p.n, blockIdx.x * p.per, end,
+                   1.0 / (sqrt(s) + (double)p.eps));
 }
 
 // small matrices: one workgroup each, in one launch
@@ -77,9 +96,7 @@ template <class E>
 __global__ __launch_bounds__(1024) void norm_scale_kernel(OrthParams p) {
     const E* const u = static_cast<const E*>(p.U) + (int64_t)blockIdx.x * p.n;
     float* const x = p.X + (int64_t)blockIdx.x * p.n;
-    const double by = 1.0 / (sqrt(sum_squares<E, 1024>(u, 0, p.n)) + (double)p.eps);
-#pragma unroll 4
-    for (int64_t i = threadIdx.x; i < p.n; i += 1024) x[i] = (float)((double)to_float(u[i]) * by);
+    scaled<E, 1024>(u, x, 0, p.n, 1.0 / (sqrt(sum_squares<E, 1024>(u, 0, p.n)) + (double)p.eps));
 }
 
 template <class E>
@@ -102,7 +119,7 @@ int32_t phase(int32_t left) { return left <= 1 ? left : left % 2 ? 3 : 2; }
 
 // A phase as its single steps, or at once: the modelled times of the products that differ.
 bool at_once_preferred(int64_t m, int64_t n, int32_t batch, int32_t steps) {
-    auto us = [&](int64_t M, int64_t N, int64_t K, int32_t b) { return plan_product(Layout::kXKt, 0, M, N, K, b, false).us; };
+    auto us = [&](int64_t M, int64_t N, int64_t K, int32_t b) { return plan_product(Layout::kXKt, 0, M, N, K, b, 1, M == N).us; };
     const double gram = us(m, m, n, batch), apply = us(n, m, m, batch), square = us(m, m, m, batch);
     const double single = steps * (gram + square + apply);
     const double at_once = gram + apply + steps * square + (steps - 1) * 2 * square +
@@ -131,14 +148,14 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
     };
     float* const X[2] = {take(batch * m * n * 4), take(batch * m * n * 4)};
     float* S[kSquares];
-    for (float*& s : S) s = take(batch * mm * 4);
+    for (float*& s : S) s = take(batch * mm * 4);  // one after another: S[1] on holds kSquares - 1 of them
 
     OrthParams q{};
     q.U = U;
     q.X = X[0];
     q.part = reinterpret_cast<double*>(at);
     q.n = m * n;
-    q.per = (q.n + kShares - 1) / kShares;
+    q.per = ((q.n + kShares - 1) / kShares + 7) / 8 * 8;
     q.eps = eps;
     hipError_t e = dtype ? normalise<uint16_t>(q, batch, stream) : normalise<float>(q, batch, stream);
 
@@ -146,7 +163,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
     base.batch = batch;
     base.splits = 1;
     base.alpha = 1.0f;
-    // alpha S1 S2 of symmetric (or commuting) m x m matrices, to Y
+    // alpha S1 S2 of symmetric (or commuting) m x m matrices, to Y, which is not R
     auto square = [&](const float* s1, const float* s2, float* y, float alpha, const float* r, float beta, float diag) {
         if (e != hipSuccess) return;
         Product p = base;
@@ -160,6 +177,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.alpha = alpha;
         p.beta = beta;
         p.diag = diag;
+        p.symmetric = 1;
         e = launch_product(Layout::kXKt, p, 0, stream);
     };
     int copy = 0;
@@ -178,7 +196,12 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.K = (int32_t)n;
         p.a_batch = p.b_batch = m * n;
         p.y_batch = mm;
-        e = launch_product(wide ? Layout::kXKt : Layout::kXtK, p, 0, stream);
+        p.symmetric = 1;
+        p.part = S[1];  // the other squares are free now
+        const Layout gram = wide ? Layout::kXKt : Layout::kXtK;
+        const ProductPlan plan = plan_product(gram, 0, m, m, n, batch, kSquares - 1, true);
+        e = launch_product(plan, gram, p, 0, stream);
+        if (e == hipSuccess && plan.splits > 1) e = launch_sum_parts(S[1], plan.splits, batch * mm, A, 0, stream);
         for (int32_t k = 0; k < now; ++k) {
             float* const P = S[3 + k % 2];
             const bool last = k + 1 == now;
@@ -202,7 +225,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
                     p.lda = p.ldb = p.ldy = m;
                     p.M = p.N = p.K = (int32_t)m;
                     p.a_batch = p.b_batch = p.y_batch = mm;
-                    e = launch_product(Layout::kXKt, p, 0, stream);
+                    e = launch_product(Layout::kXKt, p, 0, stream);  // (not symmetric: the tiles' mirror knows one Y)
                 }
                 Q = to;
             }

@@ -24,6 +24,8 @@ constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
                               {64, 64, 2, {0.26, 0.38}, 3.8}};
 constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 7.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
 
+constexpr int kSymmetricF32 = 3;  // the fp32 kernel with square tiles
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
@@ -35,20 +37,22 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 
 }  // namespace
 
-ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split) {
+ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits, bool symmetric) {
     const int64_t small_rounds = ceil_div(ceil_div(M, 32) * ceil_div(N, 32) * batch, 256);
     ProductPlan best{0, 1, (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
     const TileCost* const tiles = dtype ? kBf16 : kF32;
     const int count = dtype ? 5 : 3;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
     for (int i = 0; i < count; ++i) {
-        const int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn) * batch;
-        for (int64_t s = 1; s <= 64; s = s < 4 ? s + 1 : s + s / 4) {
+        int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn);
+        if (symmetric && !dtype && i + 1 == kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
+        n *= batch;
+        for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
             // shares of at least 4 chunks of 64, none empty, and partial sums of at most 256 MB
-            if (s > 1 && (!may_split || batch > 1 || shares < 4 * s || s * M * N > (int64_t(1) << 26))) break;
+            if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
-            if (real > 1) us += 3.0 + (double)(real * M * N) / 8e5;  // the sum of the shares
+            if (real > 1) us += 3.0 + (double)(real * batch * M * N) / 8e5;  // the sum of the shares
             if (us < best.us) best = {i + 1, (int32_t)real, us};
         }
     }
@@ -57,12 +61,13 @@ ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int
 
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {
     p.splits = plan.splits;
+    p.symmetric = p.symmetric && !dtype && plan.kernel == kSymmetricF32;
     if (plan.kernel == 0) return p.splits > 1 ? hipErrorNotSupported : launch_product_small(layout, p, dtype, stream);
     return dtype ? launch_product_bf16(layout, p, plan.kernel, stream) : launch_product_f32(layout, p, plan.kernel, stream);
 }
 
 hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream) {
-    return launch_product(plan_product(layout, dtype, p.M, p.N, p.K, p.batch, false), layout, p, dtype, stream);
+    return launch_product(plan_product(layout, dtype, p.M, p.N, p.K, p.batch, 1, p.symmetric != 0), layout, p, dtype, stream);
 }
 
 }  // namespace mec

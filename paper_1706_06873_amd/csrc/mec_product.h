@@ -26,7 +26,7 @@ struct Product {
     void* Z;         // or nullptr
     const void* R;   // or nullptr
     const float* bias;  // or nullptr
-    float* part;     // with splits > 1: splits x M x N partial sums in place of Y
+    float* part;     // with splits > 1: splits x batch x M x N partial sums in place of Y
     int64_t lda, ldb, ldy, ldz, ldr;  // elements per row as stored
     int32_t M, N, K;
     int32_t act, res_first;
@@ -39,6 +39,7 @@ struct Product {
     const void* B2;
     void* Y2;
     float diag;      // added to z where m = n
+    int32_t symmetric;  // A B and R are symmetric (fp32, no act): the 64 x 64 tiles leave out those above the diagonal
     int32_t y_bf16;  // fp32 products: Y is bf16
 
     // filled by the launch
@@ -52,7 +53,9 @@ struct ProductPlan {
     int32_t splits;
     double us;   // by the model
 };
-ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, bool may_split);
+// max_splits: as many shares as the caller has room for partial sums (batch x M x N each)
+ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
+                         bool symmetric = false);
 
 // Enqueue the product (dtype of A, B, Z, R, Y), with p.splits shares that leave their partial
 // sums where it is above 1. hipErrorNotSupported where there is no such kernel.
@@ -350,7 +353,7 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
     uint16_t* const y16 = static_cast<uint16_t*>(p.Y) + yat;
     E* const z = static_cast<E*>(p.Z) + m * p.ldz + n;
     const E* const r = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;
-    float* const q = p.part + ((int64_t)split * p.M + m) * p.N + n;
+    float* const q = p.part + (((int64_t)split * p.batch + bat) * p.M + m) * p.N + n;
     float bias[8] = {};
     if (p.bias && !part)
 #pragma unroll
@@ -442,6 +445,33 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// The mirror image of a wave's block of a symmetric Y (tile above the diagonal): register v
+// of the 32 lanes with one n holds 32 consecutive m, a run of a row of the image.
+__device__ inline void mirror(const Product& p, const floatx16& acc, int32_t m0, int32_t n0, int32_t bat, int32_t split, int lane) {
+    const int32_t m = m0 + (lane & 31);
+    if (m >= p.M) return;
+    const bool part = p.splits > 1;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int64_t n = n0 + acc_row(v, lane);
+        if (n >= p.N) continue;
+        if (part) {
+            p.part[(((int64_t)split * p.batch + bat) * p.M + n) * p.N + m] = acc[v];
+        } else {
+            float x = acc[v] * p.alpha;
+            if (p.R) x += p.beta * static_cast<const float*>(p.R)[bat * p.r_batch + n * p.ldr + m];
+            static_cast<float*>(p.Y)[bat * p.y_batch + n * p.ldy + m] = x;
+        }
+    }
+}
+// Tile t of those of a symmetric Y on and below the diagonal, row by row
+__device__ inline void tile_of_half(uint32_t t, uint32_t& mt, uint32_t& nt) {
+    mt = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    while (mt * (mt + 1) / 2 > t) --mt;  // (the root is rounded)
+    while ((mt + 1) * (mt + 2) / 2 <= t) ++mt;
+    nt = t - mt * (mt + 1) / 2;
 }
 
 // Tile t of a grid of m_tiles x n_tiles: runs of `group` rows of tiles, column by column,
