@@ -410,39 +410,42 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
                                              dtype, st), "gradients of the activation and the bias");
         if (rc != MEC_OK) return rc;
     }
-    mec::Product p{};
-    p.alpha = 1.0f;
-    p.batch = p.splits = 1;
     const void* const dz = act == MEC_ACT_NONE ? G : dZ;
     const int64_t z_pitch = act == MEC_ACT_NONE ? g_pitch : k_c;
+    mec::Product x{}, k{};
+    x.alpha = k.alpha = 1.0f;
+    x.batch = x.splits = k.batch = k.splits = 1;
+    x.A = dz;
+    x.lda = z_pitch;
+    x.B = K;
+    x.ldb = k_c;
+    x.Y = dX;
+    x.ldy = i_c;
+    x.M = (int32_t)rows;
+    x.N = i_c;
+    x.K = k_c;
+    k.A = X;
+    k.lda = x_pitch;
+    k.B = dz;
+    k.ldb = z_pitch;
+    k.Y = dK;
+    k.ldy = k_c;
+    k.M = i_c;
+    k.N = k_c;
+    k.K = (int32_t)rows;
+    k.part = part;
+    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x.M, x.N, x.K, 1, 1);
+    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k.M, k.N, k.K, 1, 64);
+    if (dX && dK && px.kernel == 0 && pk.kernel == 0)
+        return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
     if (dX) {
-        p.A = dz;
-        p.lda = z_pitch;
-        p.B = K;
-        p.ldb = k_c;
-        p.Y = dX;
-        p.ldy = i_c;
-        p.M = (int32_t)rows;
-        p.N = i_c;
-        p.K = k_c;
-        rc = hip_status(mec::launch_product(mec::Layout::kXKt, p, dtype, st), "gradient of the input");
+        rc = hip_status(mec::launch_product(px, mec::Layout::kXKt, x, dtype, st), "gradient of the input");
         if (rc != MEC_OK) return rc;
     }
     if (dK) {
-        p.A = X;
-        p.lda = x_pitch;
-        p.B = dz;
-        p.ldb = z_pitch;
-        p.Y = dK;
-        p.ldy = k_c;
-        p.M = i_c;
-        p.N = k_c;
-        p.K = (int32_t)rows;
-        p.part = part;
-        const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, 64);
-        rc = hip_status(mec::launch_product(plan, mec::Layout::kXtK, p, dtype, st), "gradient of the kernel");
-        if (rc == MEC_OK && plan.splits > 1)
-            rc = hip_status(mec::launch_sum_parts(part, plan.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
+        rc = hip_status(mec::launch_product(pk, mec::Layout::kXtK, k, dtype, st), "gradient of the kernel");
+        if (rc == MEC_OK && pk.splits > 1)
+            rc = hip_status(mec::launch_sum_parts(part, pk.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
     }
     return rc;
 }

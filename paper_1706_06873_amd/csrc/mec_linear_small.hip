@@ -41,10 +41,10 @@ struct Place {
     int32_t m0, n0, bat, waves;
     Slice k;
 };
-__device__ inline Place place(const Product& p, int wave) {
+// tile `b` of all of p's
+__device__ inline Place place(const Product& p, uint32_t b, int wave) {
     Place t;
     const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
-    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
     t.bat = (int32_t)(b / tiles);
     const uint32_t r = b - (uint32_t)t.bat * tiles, mt = r / (uint32_t)p.n_tiles;
     t.m0 = (int32_t)mt * 32;
@@ -84,12 +84,11 @@ __device__ inline void fetch(const float* base, int64_t ld, int32_t k, int32_t k
 }
 
 template <Layout L>
-__global__ __launch_bounds__(64 * kWaves) void small_f32_kernel(Product p) {
+__device__ inline void small_f32(const Product& p, uint32_t b0, float* sums) {
     constexpr bool AT = L == Layout::kXtK, BT = L != Layout::kXKt;
     constexpr int U = 2;  // steps of 16 k in flight
-    __shared__ __align__(16) float sums[kWaves * 32 * kPitch];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place t = place(p, wave);
+    const Place t = place(p, b0, wave);
     floatx16 acc = {};
     if (wave < t.waves) {
         // rows and columns past the last are copies of it
@@ -200,14 +199,18 @@ struct Turn {
     }
 };
 
+template <Layout L>
+constexpr int kPatches = (L == Layout::kXtK ? kPatch : 0) + (L != Layout::kXKt ? kPatch : 0);  // of a wave
+constexpr int kSums = kWaves * 32 * kPitch * 4;
+template <Layout L>
+constexpr int kLds = kWaves * kPatches<L> > kSums ? kWaves * kPatches<L> : kSums;
+
 template <Layout L, bool CLEAN>
-__global__ __launch_bounds__(64 * kWaves) void small_bf16_kernel(Product p) {
+__device__ inline void small_bf16(const Product& p, uint32_t b0, char* lds) {
     constexpr bool AT = L == Layout::kXtK, BT = L != Layout::kXKt;
-    constexpr int PATCHES = (AT ? kPatch : 0) + (BT ? kPatch : 0);
-    constexpr int SUMS = kWaves * 32 * kPitch * 4;
-    __shared__ __align__(16) char lds[kWaves * PATCHES > SUMS ? kWaves * PATCHES : SUMS];
+    constexpr int PATCHES = kPatches<L>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place t = place(p, wave);
+    const Place t = place(p, b0, wave);
     floatx16 acc = {};
     if (wave < t.waves) {
         const uint16_t* const a = a_of<uint16_t>(p, t.bat) + (AT ? (int64_t)t.m0 : t.m0 * p.lda);
@@ -247,21 +250,44 @@ __global__ __launch_bounds__(64 * kWaves) void small_bf16_kernel(Product p) {
     join<uint16_t>(p, acc, reinterpret_cast<float*>(lds), t.m0, t.n0, t.bat, t.waves, wave, lane);
 }
 
+// One product, or (pair) the two of a backward pass, dX = dZ K^T and dK = X^T dZ, side by side
+// in one launch: the launch is what a small pass waits for (3 us of host time each).
 template <Layout L>
-hipError_t run(const Product& p, int dtype, hipStream_t stream) {
-    const dim3 grid((uint32_t)((int64_t)p.m_tiles * p.n_tiles * p.batch)), block(64 * kWaves);
+__global__ __launch_bounds__(64 * kWaves) void small_f32_kernel(Product p) {
+    __shared__ __align__(16) float sums[kWaves * 32 * kPitch];
+    small_f32<L>(p, xcd_remap(blockIdx.x, gridDim.x), sums);
+}
+__global__ __launch_bounds__(64 * kWaves) void small_f32_pair_kernel(Product x, Product k, uint32_t x_blocks) {
+    __shared__ __align__(16) float sums[kWaves * 32 * kPitch];
+    if (blockIdx.x < x_blocks) small_f32<Layout::kXKt>(x, xcd_remap(blockIdx.x, x_blocks), sums);
+    else small_f32<Layout::kXtK>(k, blockIdx.x - x_blocks, sums);
+}
+template <Layout L, bool CLEAN>
+__global__ __launch_bounds__(64 * kWaves) void small_bf16_kernel(Product p) {
+    __shared__ __align__(16) char lds[kLds<L>];
+    small_bf16<L, CLEAN>(p, xcd_remap(blockIdx.x, gridDim.x), lds);
+}
+template <bool CLEAN>
+__global__ __launch_bounds__(64 * kWaves) void small_bf16_pair_kernel(Product x, Product k, uint32_t x_blocks) {
+    __shared__ __align__(16) char lds[kLds<Layout::kXtK>];
+    if (blockIdx.x < x_blocks) small_bf16<Layout::kXKt, CLEAN>(x, xcd_remap(blockIdx.x, x_blocks), lds);
+    else small_bf16<Layout::kXtK, CLEAN>(k, blockIdx.x - x_blocks, lds);
+}
+
+template <Layout L>
+hipError_t run(const Product& p, int dtype, uint32_t blocks, hipStream_t stream) {
+    const dim3 grid(blocks), block(64 * kWaves);
     if (!dtype) hipLaunchKernelGGL(small_f32_kernel<L>, grid, block, 0, stream, p);
     else if (p.clean) hipLaunchKernelGGL((small_bf16_kernel<L, true>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((small_bf16_kernel<L, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
-}  // namespace
-
-hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream) {
+// Fills what the kernels need; the workgroups, or 0 past the grid.
+uint32_t prepare(Product& p, Layout layout, int dtype) {
     p.m_tiles = (p.M + 31) / 32;
     p.n_tiles = (p.N + 31) / 32;
-    if ((int64_t)p.m_tiles * p.n_tiles * p.batch > 0x3fffff || p.splits > 1) return hipErrorInvalidValue;
+    const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * p.batch;
     // a wave's run: whole steps of 16 k
     const int64_t steps = ((int64_t)p.K + 15) / 16;
     p.chunks = (int32_t)((steps + kWaves - 1) / kWaves);
@@ -270,11 +296,29 @@ hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t
         p.clean = !(((uintptr_t)p.A | (uintptr_t)p.B) & 15u) && p.lda % 8 == 0 && p.ldb % 8 == 0 && a_run % 8 == 0 &&
                   b_run % 8 == 0 && p.a_batch % 8 == 0 && p.b_batch % 8 == 0;
     }
+    return blocks > 0x1fffff || p.splits > 1 ? 0 : (uint32_t)blocks;
+}
+
+}  // namespace
+
+hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream) {
+    const uint32_t blocks = prepare(p, layout, dtype);
+    if (!blocks) return hipErrorInvalidValue;
     switch (layout) {
-        case Layout::kXK: return run<Layout::kXK>(p, dtype, stream);
-        case Layout::kXKt: return run<Layout::kXKt>(p, dtype, stream);
-        default: return run<Layout::kXtK>(p, dtype, stream);
+        case Layout::kXK: return run<Layout::kXK>(p, dtype, blocks, stream);
+        case Layout::kXKt: return run<Layout::kXKt>(p, dtype, blocks, stream);
+        default: return run<Layout::kXtK>(p, dtype, blocks, stream);
     }
+}
+
+hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream) {
+    const uint32_t bx = prepare(x, Layout::kXKt, dtype), bk = prepare(k, Layout::kXtK, dtype);
+    if (!bx || !bk) return hipErrorInvalidValue;
+    const dim3 grid(bx + bk), block(64 * kWaves);
+    if (!dtype) hipLaunchKernelGGL(small_f32_pair_kernel, grid, block, 0, stream, x, k, bx);
+    else if (x.clean && k.clean) hipLaunchKernelGGL(small_bf16_pair_kernel<true>, grid, block, 0, stream, x, k, bx);
+    else hipLaunchKernelGGL(small_bf16_pair_kernel<false>, grid, block, 0, stream, x, k, bx);
+    return hipGetLastError();
 }
 
 }  // namespace mec

@@ -63,6 +63,8 @@ hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int
 hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream);  // mec_linear.hip
 hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream);   // mec_linear_f32.hip
 hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream);  // mec_linear_small.hip
+// two small products, x of layout kXKt and k of kXtK, in one launch
+hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream);
 // by the plan, in one share
 hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream);
 
