@@ -4,6 +4,7 @@
     python -m paper_1706_06873_amd.suite stride [--batch 32] [--dtype f32]
     python -m paper_1706_06873_amd.suite resnet101 [--batch 1] [--dtype f32]
     python -m paper_1706_06873_amd.suite train [--layers resnet_mid,cv9,...] [--yardstick]
+    python -m paper_1706_06873_amd.suite block [--batch 32] [--dtype f32|bf16|both] [--layers cv9,...]
 
 ``table2`` runs the twelve layers of Table 2 (cv1-cv12), ``stride`` runs cv1
 (227x227x3 input, 11x11x96 kernel) with s_h = s_w = 1..10 as in Fig. 4(a),
@@ -16,7 +17,11 @@ products against K and the fold (the input gradient's general path; layers
 taking the sub-pixel phases of the padded gradient run those instead), the
 lowering and the partial A_h^T G_h sums with their reduction; with
 ``--yardstick`` it also times torch's own convolution gradients (the vendor
-library) on the same shapes in NCHW, for context. ``table2 --yardstick`` (and
+library) on the same shapes in NCHW, for context. ``block`` times the layer
+operators as a training step of a network has them, on the output of each of Table 2's
+stride-1 3x3 layers (cv6-cv12): layer norm, a widening ``linear`` (to four times
+the channels, GELU), a narrowing one with the residual, the gradients of the three, and
+the orthogonalised update of the layer's own kernel. ``table2 --yardstick`` (and
 the other forward modes) also times the vendor GEMM (hipBLASLt through torch)
 on the same im2col matrix, for context: im2col + vendor GEMM.
 For every layer it times MEC from L (compact lowering + slab products), MEC
@@ -176,6 +181,80 @@ def _time_layer(layer, reps, warmup, sets, yardstick=False, settle=0.2):
                                                                        res["fused"]["us"]), 3)}
 
 
+def _median_us(steps, stream, reps, warmup):
+    """The median time of each step (name -> call on `stream`) between HIP events, in us."""
+    times = {}
+    with torch.cuda.stream(stream):
+        for name, fn in steps.items():
+            for _ in range(warmup):
+                fn()
+            torch.cuda.synchronize()
+            ev = [(HipEvent(), HipEvent())
+                  for _ in range(reps)]
+            for a, b in ev:
+                a.record(stream)
+                fn()
+                b.record(stream)
+            torch.cuda.synchronize()
+            t = sorted(a.elapsed_time(b) * 1e3 for a, b in ev)
+            times[name] = round(t[len(t) // 2], 2)
+    return times
+
+
+def block_layers():
+    """Table 2's stride-1 3x3 layers."""
+    return [n for n in wl.TABLE2 if wl.table2_layer(n, 1).dims[4:6] == (3, 3)
+            and wl.table2_layer(n, 1).dims[7:] == (1, 1)]
+
+
+def _time_block(layer, dtype, reps, warmup):
+    """The layer operators on the output of `layer` (i_n x o_h x o_w x c), as a residual block
+    runs them: Y = X + linear(gelu(linear(norm(X)))), its gradients, and K's update."""
+    i_n, i_h, i_w, i_c, k_h, k_w, c, s_h, s_w = layer.dims
+    o_h, o_w = mec.output_dims(i_h, i_w, k_h, k_w, s_h, s_w)
+    dev = torch.device("cuda:0")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device=dev).manual_seed(layer.seed + 11)
+    randn = lambda *shape: torch.randn(shape, generator=g, device=dev)  # noqa: E731
+    rows, wide = i_n * o_h * o_w, 4 * c
+    X, G = randn(i_n, o_h, o_w, c).to(dt), randn(i_n, o_h, o_w, c).to(dt)
+    gamma, beta = 1 + 0.1 * randn(c), 0.1 * randn(c)
+    K1, b1 = (randn(c, wide) / c ** 0.5).to(dt), 0.1 * randn(wide)
+    K2, b2 = (randn(wide, c) / wide ** 0.5).to(dt), 0.1 * randn(c)
+    dK = 1e-3 * randn(k_h, k_w, i_c, c)
+    stream = torch.cuda.Stream(device=dev)
+    code = mec.BF16 if dtype == "bf16" else mec.F32
+    ws = torch.empty(max(mec.linear_grad_workspace_bytes(rows, c, wide, code),
+                         mec.linear_grad_workspace_bytes(rows, wide, c, code),
+                         mec.layer_norm_grad_workspace_bytes(rows, c, code),
+                         mec.orthogonalize_workspace_bytes(1, k_h * k_w * i_c, c)), dtype=torch.uint8, device=dev)
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        N, mean, rstd = mec.layer_norm(X, gamma, beta)
+        Z = torch.empty((i_n, o_h, o_w, wide), dtype=dt, device=dev)
+        H = mec.linear(N, K1, b1, act="gelu", Z=Z)
+        Y = torch.empty_like(X)
+        dH, dZ, dX = torch.empty_like(H), torch.empty_like(Z), torch.empty_like(X)
+        dK1, dK2, O = torch.empty_like(K1), torch.empty_like(K2), torch.empty_like(dK)
+        dg, db, db1, db2 = (torch.empty_like(t) for t in (gamma, beta, b1, b2))
+    steps = {
+        "norm": lambda: mec.layer_norm(X, gamma, beta, Y=N, mean=mean, rstd=rstd),
+        "widen": lambda: mec.linear(N, K1, b1, act="gelu", Y=H, Z=Z),
+        "narrow": lambda: mec.linear(H, K2, b2, residual=X, Y=Y),
+        "narrow_grad": lambda: mec.linear_grad(G, H, K2, dX=dH, dK=dK2, dbias=db2, workspace=ws),
+        "widen_grad": lambda: mec.linear_grad(dH, N, K1, Z, "gelu", dZ=dZ, dX=dX, dK=dK1, dbias=db1, workspace=ws),
+        "norm_grad": lambda: mec.layer_norm_grad(G, X, mean, rstd, gamma, dX=dX, dgamma=dg, dbeta=db, workspace=ws),
+        "update": lambda: mec.orthogonalize(dK, O=O, workspace=ws),
+    }
+    times = _median_us(steps, stream, reps, warmup)
+    tf = lambda us, n: round(2.0 * n * rows * c * wide / us / 1e6, 2)  # noqa: E731
+    return {"layer": layer.name, "dtype": dtype, "pixels": rows, "channels": c, "wide": wide, "us": times,
+            "widen_tflops": tf(times["widen"], 1), "narrow_tflops": tf(times["narrow"], 1),
+            "widen_grad_tflops": tf(times["widen_grad"], 2), "narrow_grad_tflops": tf(times["narrow_grad"], 2),
+            "norm_tbps": round(2.0 * X.numel() * X.element_size() / times["norm"] / 1e6, 3),
+            "norm_grad_tbps": round(3.0 * X.numel() * X.element_size() / times["norm_grad"] / 1e6, 3)}
+
+
 def _time_train(layer, reps, warmup, yardstick):
     i_n, i_h, i_w, i_c, k_h, k_w, k_c, s_h, s_w = layer.dims
     o_h, o_w = mec.output_dims(i_h, i_w, k_h, k_w, s_h, s_w)
@@ -212,21 +291,7 @@ def _time_train(layer, reps, warmup, yardstick):
         Gn = G.permute(0, 3, 1, 2).contiguous()
         steps["vendor_dgrad"] = lambda: torch.nn.grad.conv2d_input(In.shape, Kn, Gn, stride=(s_h, s_w))
         steps["vendor_wgrad"] = lambda: torch.nn.grad.conv2d_weight(In, Kn.shape, Gn, stride=(s_h, s_w))
-    times = {}
-    with torch.cuda.stream(stream):
-        for name, fn in steps.items():
-            for _ in range(warmup):
-                fn()
-            torch.cuda.synchronize()
-            ev = [(HipEvent(), HipEvent())
-                  for _ in range(reps)]
-            for a, b in ev:
-                a.record(stream)
-                fn()
-                b.record(stream)
-            torch.cuda.synchronize()
-            t = sorted(a.elapsed_time(b) * 1e3 for a, b in ev)
-            times[name] = round(t[len(t) // 2], 2)
+    times = _median_us(steps, stream, reps, warmup)
     tf = lambda us: round(2.0 * macs / (us * 1e-6) / 1e12, 2)
     out = {"layer": layer.name, "dims": list(layer.dims), "gflop": round(2.0 * macs / 1e9, 3),
            "us": times,
@@ -247,7 +312,7 @@ def _time_train(layer, reps, warmup, yardstick):
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("which", choices=["table2", "stride", "resnet101", "train"])
+    ap.add_argument("which", choices=["table2", "stride", "resnet101", "train", "block"])
     ap.add_argument("--yardstick", action="store_true",
                     help="train: also time torch's convolution gradients; forward modes: "
                          "the vendor GEMM on the im2col matrix")
@@ -277,6 +342,11 @@ def main(argv=None):
                 layer = dataclasses.replace(layer, i_n=args.batch)
             print(json.dumps(_time_train(layer, args.reps, args.warmup, args.yardstick)),
                   flush=True)
+        return 0
+    if args.which == "block":
+        for name in args.layers.split(",") if args.layers else block_layers():
+            for d in dtypes:
+                print(json.dumps(_time_block(wl.table2_layer(name, batch), d, args.reps, args.warmup)), flush=True)
         return 0
     if args.which == "table2":
         names = args.layers.split(",") if args.layers else list(wl.TABLE2)

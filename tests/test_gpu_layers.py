@@ -499,3 +499,14 @@ def test_a_given_stream_owns_what_the_call_allocates():
         for a, b in zip(want, got):
             assert torch.equal(a, b)
         del busy
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_suites_block(capsys, dtype):
+    import json
+    from paper_1706_06873_amd import suite
+    assert suite.main(["block", "--layers", "cv12", "--batch", "2", "--dtype", dtype, "--reps", "2", "--warmup", "1"]) == 0
+    row = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert row["layer"] == "cv12" and row["dtype"] == dtype and row["wide"] == 4 * row["channels"]
+    assert set(row["us"]) == {"norm", "widen", "narrow", "narrow_grad", "widen_grad", "norm_grad", "update"}
+    assert all(t > 0 for t in row["us"].values())

@@ -6,6 +6,7 @@ import ctypes
 import pytest
 import torch
 
+import kernels as kn
 import paper_1706_06873_amd as mec
 
 FAKE, ODD, NULL = ctypes.c_void_p(0x100000), ctypes.c_void_p(0x100001), None
@@ -186,3 +187,35 @@ def test_binding_refuses_updates():
         mec.orthogonalize(_t(4, 4), workspace=_t(8, dtype=torch.uint8))
     with pytest.raises(mec.MecError):
         mec.orthogonalize(_t(0, 4))
+
+
+# ---------------------------------------------------------------- which kernel a product takes
+
+@pytest.mark.parametrize("layout,dtype,M,N,K,batch,split,want", [
+    (kn.XK, "bf16", 1, 1000, 2048, 1, False, (0, 1)),          # few outputs: the waves share the reduction
+    (kn.XK, "f32", 333, 131, 363, 1, False, (0, 1)),
+    (kn.XK, "bf16", 16384, 4096, 4096, 1, False, (2, 1)),      # 256 x 256 tiles
+    (kn.XK, "f32", 16384, 4096, 1024, 1, False, (2, 1)),       # 256 x 128
+    (kn.XK, "f32", 100352, 256, 64, 1, False, (1, 1)),         # short reductions: tiles that overlap
+    (kn.XKT, "bf16", 1024, 1024, 1024, 1, False, (5, 1)),      # 64 x 64, a tile per compute unit
+])
+def test_product_plans(layout, dtype, M, N, K, batch, split, want):
+    assert kn.product_plan(layout, dtype, M, N, K, batch, split) == want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_product_plans_share_long_reductions(dtype):
+    kernel, shares = kn.product_plan(kn.XTK, dtype, 512, 2048, 50176, 1, True)
+    assert kernel > 0 and 4 <= shares <= 64
+    assert kn.product_plan(kn.XTK, dtype, 512, 2048, 50176, 1, False)[1] == 1
+    for M, N, K in ((1, 1, 1), (7, 3, 1 << 20), (64, 64, 100000), (1 << 20, 1, 3), (4096, 4096, 131072), (200, 100, 1000)):
+        kernel, shares = kn.product_plan(kn.XTK, dtype, M, N, K, 1, True)
+        runs = -(-K // 64)
+        assert 1 <= shares <= max(1, runs // 4) and (shares - 1) * (-(-runs // shares)) < runs  # none empty
+        assert shares * M * N <= max(M * N, 1 << 26)
+
+
+def test_the_suites_block_layers():
+    from paper_1706_06873_amd import suite
+    layers = suite.block_layers()
+    assert "cv12" in layers and "cv1" not in layers and len(layers) >= 5
