@@ -150,12 +150,13 @@ hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream)
 }
 
 // Few rows (one share): 64 at a time, so that the column sums need no second launch. Else
-// strips of up to 1024 columns, as narrow as hold the row.
+// strips of 1024 columns where those fill the GPU, or of 256 (800 rows of 2048 in bf16, 25
+// shares: 21 us in wide strips, so 10) or 128.
 template <class E>
 hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
     if (shares == 1) return act_grad<E, 16, 1024>(p, shares, stream);
-    return p.N > 512 ? act_grad<E, 128, 256>(p, shares, stream)
-                     : p.N > 128 ? act_grad<E, 32, 256>(p, shares, stream) : act_grad<E, 16, 256>(p, shares, stream);
+    if (p.N > 512 && (int64_t)shares * ((p.N + 1023) / 1024) >= 512) return act_grad<E, 128, 256>(p, shares, stream);
+    return p.N > 128 ? act_grad<E, 32, 256>(p, shares, stream) : act_grad<E, 16, 256>(p, shares, stream);
 }
 
 }  // namespace

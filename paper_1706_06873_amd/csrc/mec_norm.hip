@@ -32,7 +32,7 @@ struct NormParams {
 
 // V consecutive elements (16 bytes' worth) at any boundary of the element's size, of which
 // `have` are the row's; the others come as zeros and are not written. (The same instructions
-// as for 16-byte rows; single elements took 725 us where these take 180, 108934 rows of 1619
+// as for 16-byte rows; single elements took 725 us where these take 221, 108934 rows of 1619
 // in bf16.)
 struct __attribute__((packed, aligned(4))) AnyF {
     f32x4v v;
@@ -401,7 +401,7 @@ hipError_t launch_norm(const void* X, int64_t ldx, const float* gamma, const flo
 }
 
 // Workgroups of the backward pass, each of which leaves 2 C partial sums: one per row up to
-// 256 (49 rows of 2048: one per 16 rows 20 us, so 9), then one per 16 rows, so that the
+// 256 (49 rows of 2048: one per 16 rows 18.5 us, so 7.5), then one per 16 rows, so that the
 // partial sums stay a small part of the traffic, up to 1024.
 int64_t norm_grad_blocks(int64_t rows) {
     const int64_t few = rows < 256 ? rows : 256, many = (rows + 15) / 16;

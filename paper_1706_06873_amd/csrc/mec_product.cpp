@@ -22,7 +22,7 @@ constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
                               {64, 128, 3, {0.40, 0.70, 0.85}, 3.5},
                               {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4},
                               {64, 64, 2, {0.26, 0.38}, 3.8}};
-constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 10.5}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
+constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
 
 constexpr int kSymmetricF32 = 3;  // the fp32 kernel with square tiles
 
