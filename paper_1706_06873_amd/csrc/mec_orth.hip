@@ -5,16 +5,17 @@
 // step in the directions of small singular values, 140 times over the steps after the
 // first, which fp32 has room for and bf16 (2^-9 a rounding) has not.
 //
-// Several steps at once: with P = a I + b A + c A^2 the Gram matrix after the step is P A P,
-// so a phase of s steps needs one Gram matrix of X and one product with X, for Q = P_s .. P_1,
-// and the rest on m x m matrices (which commute, being polynomials of A): A^2, P A, (P A) P
-// and P Q. In products of m x m x m that is 2r + 5 against 4r + 2 for 2 steps and 2r + 9
-// against 6r + 3 for 3. The error of A is relative to its largest value, and a phase
-// multiplies it in the small singular directions, so phases are short and the longest comes
-// first, where the singular values are smallest and all still far from the polynomial's
-// range: 3 + 2 steps stay within 1.3 of the single steps' error against 64 bits (2e-6 to
-// 1.6e-5 over Gaussian, low-rank and log-spaced spectra down to 1e-6), 5 at once lose up to
-// 70 times.
+// Two steps at once: with P = a I + b A + c A^2 the Gram matrix after the step is P A P, so a
+// pair of steps needs one Gram matrix of X and one product with X, for P' P, and the rest on
+// m x m matrices (which commute, being polynomials of A): P A, (P A) P and P' P. In products
+// of m x m x m that is 2r + 5 against 4r + 2. The error of A is relative to its largest value,
+// and a step multiplies it in the small singular directions, so a pair costs nothing where
+// all singular values are alike or what it spoils is not multiplied again: the first two
+// steps (all below the polynomial's range yet) and the last two. The steps between them are
+// taken one by one. With 5 steps, 2 + 1 + 2 stay within 1.7 of the single steps' error
+// against 64 bits (1.1 at the median; 4e-7 to 4e-5 over Gaussian, low-rank, log-spaced and
+// two-valued spectra of 16 x 64 to 200 x 400); 1 + 2 + 2 lose up to 6 times, 3 + 2 up to 12
+// (thin matrices), 5 at once up to 70.
 #include "mec_product.h"
 
 namespace mec {
@@ -112,19 +113,14 @@ hipError_t normalise(const OrthParams& q, int32_t batch, hipStream_t stream) {
 
 int64_t round16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
-constexpr int kSquares = 7;  // m x m matrices of a phase, for each of the stack
+// m x m matrices for each of the stack: A, A after a step, P A (then P' P), P, P'; before the
+// first of them all but A hold the shares of its sum.
+constexpr int kSquares = 7;
 
-// Steps of the phase that begins with `left` steps to go.
-int32_t phase(int32_t left) { return left <= 1 ? left : left % 2 ? 3 : 2; }
-
-// A phase as its single steps, or at once: the modelled times of the products that differ.
-bool at_once_preferred(int64_t m, int64_t n, int32_t batch, int32_t steps) {
-    auto us = [&](int64_t M, int64_t N, int64_t K, int32_t b) { return plan_product(Layout::kXKt, 0, M, N, K, b, 1, M == N).us; };
-    const double gram = us(m, m, n, batch), apply = us(n, m, m, batch), square = us(m, m, m, batch);
-    const double single = steps * (gram + square + apply);
-    const double at_once = gram + apply + steps * square + (steps - 1) * 2 * square +
-                           (steps > 1 ? (steps - 2) * (us(m, m, m, 2 * batch) - square) + square : 0.0);
-    return at_once < single;
+// A pair of steps at once: the modelled times of the products that differ.
+bool pairs_preferred(int64_t m, int64_t n, int32_t batch) {
+    auto us = [&](int64_t M, int64_t N, int64_t K) { return plan_product(Layout::kXKt, 0, M, N, K, batch, 1, M == N).us; };
+    return us(m, m, n) + us(n, m, m) > 3 * us(m, m, m);
 }
 
 }  // namespace
@@ -181,11 +177,11 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         e = launch_product(Layout::kXKt, p, 0, stream);
     };
     int copy = 0;
-    const bool group = at_once_preferred(m, n, batch, 2);
+    const bool pairs = pairs_preferred(m, n, batch);
     for (int32_t left = steps; left > 0 && e == hipSuccess;) {
-        const int32_t now = group ? phase(left) : 1;
-        left -= now;
-        float *A = S[0], *A2 = S[1], *const T = S[2], *Q = nullptr;
+        const bool two = pairs && left >= 2 && (left == steps || left == 2);
+        left -= two ? 2 : 1;
+        float *const A = S[0], *const A2 = S[1], *const T = S[2], *const P = S[3], *const P2 = S[4];
         const float* const from = X[copy];
         Product p = base;  // A
         p.A = p.B = from;
@@ -202,43 +198,17 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         const ProductPlan plan = plan_product(gram, 0, m, m, n, batch, kSquares - 1, true);
         e = launch_product(plan, gram, p, 0, stream);
         if (e == hipSuccess && plan.splits > 1) e = launch_sum_parts(S[1], plan.splits, batch * mm, A, 0, stream);
-        for (int32_t k = 0; k < now; ++k) {
-            float* const P = S[3 + k % 2];
-            const bool last = k + 1 == now;
-            square(A, A, P, c, A, b, now > 1 ? a : 0.0f);  // the single step adds a X itself
-            if (k == 0) {
-                Q = P;
-                if (!last) square(P, A, T, 1.0f, nullptr, 0.0f, 0.0f);
-            } else if (e == hipSuccess) {
-                float* const to = S[5 + k % 2];
-                if (last) {
-                    square(P, Q, to, 1.0f, nullptr, 0.0f, 0.0f);
-                } else {  // P A and P Q in one launch
-                    p = base;
-                    p.A = P;
-                    p.B = A;
-                    p.B2 = Q;
-                    p.Y = T;
-                    p.Y2 = to;
-                    p.half = batch;
-                    p.batch = 2 * batch;
-                    p.lda = p.ldb = p.ldy = m;
-                    p.M = p.N = p.K = (int32_t)m;
-                    p.a_batch = p.b_batch = p.y_batch = mm;
-                    e = launch_product(Layout::kXKt, p, 0, stream);  // (not symmetric: the tiles' mirror knows one Y)
-                }
-                Q = to;
-            }
-            if (!last) {
-                square(T, P, A2, 1.0f, nullptr, 0.0f, 0.0f);
-                float* const s = A;
-                A = A2;
-                A2 = s;
-            }
+        square(A, A, P, c, A, b, two ? a : 0.0f);  // a single step adds a X itself
+        if (two) {
+            square(P, A, T, 1.0f, nullptr, 0.0f, 0.0f);
+            square(T, P, A2, 1.0f, nullptr, 0.0f, 0.0f);
+            square(A2, A2, P2, c, A2, b, a);
+            square(P2, P, T, 1.0f, nullptr, 0.0f, 0.0f);
         }
+        const float* const Q = two ? T : P;
         if (e != hipSuccess) break;
         p = base;  // X
-        if (now == 1) {
+        if (!two) {
             p.R = from;
             p.beta = a;
         }

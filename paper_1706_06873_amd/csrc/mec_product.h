@@ -34,10 +34,6 @@ struct Product {
     int32_t splits;  // of the reduction
     int32_t batch;   // equal products, the strides below apart (elements)
     int64_t a_batch, b_batch, y_batch, r_batch;
-    // half != 0: the products from `half` on take A's from the start again, and B2 and Y2
-    int32_t half;
-    const void* B2;
-    void* Y2;
     float diag;      // added to z where m = n
     int32_t symmetric;  // A B and R are symmetric (fp32, no act): the 64 x 64 tiles leave out those above the diagonal
     int32_t y_bf16;  // fp32 products: Y is bf16
@@ -263,21 +259,19 @@ __device__ inline void finish(const Product& p, int64_t m, int32_t n, int32_t ba
     else if (p.act == kActSilu) v = act_value<FAST>(kActSilu, v);
     else if (p.act == kActGelu) v = act_value<FAST>(kActGelu, v);
     if (p.R && !p.res_first) v += r;
-    const bool second = p.half && bat >= p.half;
-    const int64_t at = (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
+    const int64_t at = bat * p.y_batch + m * p.ldy + n;
     if (sizeof(E) == 4 && p.y_bf16) static_cast<uint16_t*>(p.Y)[at] = from_float<uint16_t>(v);
-    else static_cast<E*>(second ? p.Y2 : p.Y)[at] = from_float<E>(v);
+    else static_cast<E*>(p.Y)[at] = from_float<E>(v);
 }
 
 // the operands of product `bat` of a batch
 template <class E>
 __device__ inline const E* a_of(const Product& p, int32_t bat) {
-    return static_cast<const E*>(p.A) + (p.half && bat >= p.half ? bat - p.half : bat) * p.a_batch;
+    return static_cast<const E*>(p.A) + bat * p.a_batch;
 }
 template <class E>
 __device__ inline const E* b_of(const Product& p, int32_t bat) {
-    return p.half && bat >= p.half ? static_cast<const E*>(p.B2) + (bat - p.half) * p.b_batch
-                                   : static_cast<const E*>(p.B) + bat * p.b_batch;
+    return static_cast<const E*>(p.B) + bat * p.b_batch;
 }
 
 // 8 elements as they lie in memory, at any boundary of the element's size
@@ -347,11 +341,11 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
     const int row0 = lane / LPR, col = (lane % LPR) * 8;
     const int32_t have = p.N - n0 - col;  // columns from this lane's first on
     const int32_t rows = p.M - m0 - row0;
-    const bool part = p.splits > 1, diagonal = p.diag != 0.0f, second = p.half && bat >= p.half;
+    const bool part = p.splits > 1, diagonal = p.diag != 0.0f;
     const bool half = sizeof(E) == 4 && p.y_bf16;
     const int64_t m = m0 + row0, n = n0 + col;
-    const int64_t yat = (second ? bat - p.half : bat) * p.y_batch + m * p.ldy + n;
-    E* const y = static_cast<E*>(second ? p.Y2 : p.Y) + yat;
+    const int64_t yat = bat * p.y_batch + m * p.ldy + n;
+    E* const y = static_cast<E*>(p.Y) + yat;
     uint16_t* const y16 = static_cast<uint16_t*>(p.Y) + yat;
     E* const z = static_cast<E*>(p.Z) + m * p.ldz + n;
     const E* const r = static_cast<const E*>(p.R) + bat * p.r_batch + m * p.ldr + n;

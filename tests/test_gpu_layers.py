@@ -364,6 +364,28 @@ def test_orthogonalize(dtype, batch, rows, cols):
     assert torch.equal(mec.orthogonalize(Ud, O=Ud), O) and torch.equal(Ud, O)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(6, 2016, 53), (2, 32, 2160), (1, 50, 260), (3, 128, 1152), (1, 200, 400)])
+@pytest.mark.parametrize("noise", [1.0, 0.3, 0.03])
+def test_orthogonalize_as_precise_as_single_steps(batch, rows, cols, noise):
+    """Steps taken two at once form the second Gram matrix from two products more of the small
+    side, each with the roundings of one: at most twice the error of plain steps in fp32."""
+    g = torch.Generator().manual_seed(rows)
+    k = max(1, min(rows, cols) // 8)
+    U = randn(g, batch, rows, k) @ randn(g, batch, k, cols) / k ** 0.5 * (noise < 1) + noise * randn(g, batch, rows, cols)
+    print("[case]", batch, rows, cols, noise, flush=True)
+    want = orth64(U)
+    a, b, c = 3.4445, -4.7750, 2.0315
+    X = U / (U.flatten(1).norm(dim=1).view(-1, 1, 1) + 1e-7)
+    X = X.mT.contiguous() if rows > cols else X
+    for _ in range(5):
+        A = X @ X.mT.contiguous()
+        X = a * X + (b * A + c * (A @ A)) @ X
+    plain = X.mT if rows > cols else X
+    got = mec.orthogonalize(U.to(DEV)).cpu()
+    err = lambda x: ((x.double() - want).norm() / want.norm()).item()
+    assert err(got) <= max(1e-6, 2 * err(plain)), (err(got), err(plain))
+
+
 def test_orthogonalize_shapes_scales_and_zeros():
     g = torch.Generator().manual_seed(4)
     dK = randn(g, 3, 3, 16, 24).to(DEV)
