@@ -342,7 +342,8 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
  * dbias may each be NULL: not wanted (X is then read for dK, K for dX alone). With
  * MEC_ACT_NONE dZ is G: Z and dZ may be NULL and are not touched; otherwise dZ is
  * always written, and products take it as rounded to dtype; it may be Z's memory,
- * or G's where g_pitch = k_c.
+ * or G's where g_pitch = k_c. Otherwise outputs must overlap neither each other nor
+ * the inputs.
  * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for the partial sums of
  * dK and dbias; may be NULL where neither is wanted. */
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);

@@ -36,6 +36,7 @@ LIB_PATH = os.path.join(_HERE, "libmec.so")
 F32, BF16 = 0, 1
 LOWERED, FUSED, IM2COL = 0, 1, 2
 GRAD_INPUT, GRAD_KERNEL, GRAD_KERNEL_FROM_L = 0, 1, 2
+_UNSUPPORTED = -5  # MEC_ERR_UNSUPPORTED
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _ALGOS = {"lowered": LOWERED, "fused": FUSED, "im2col": IM2COL,
           LOWERED: LOWERED, FUSED: FUSED, IM2COL: IM2COL}
@@ -499,6 +500,13 @@ def _pitch(t, name, c):
     raise ValueError("%s must be contiguous, or rows of contiguous channels" % name)
 
 
+def _width(*sizes):
+    """Sizes past the C interface's int are refused here, the others there."""
+    for n in sizes:
+        if n > 0x7fffffff:
+            raise MecError(_UNSUPPORTED, "a size of %d" % n)
+
+
 def _channels(t, name):
     """(shape, rows, channels) of activations, and their dtype's code."""
     shape = t.shape
@@ -508,6 +516,7 @@ def _channels(t, name):
     if dt is None:
         raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
     c = shape[-1]
+    _width(c)
     return shape, (t.numel() // c if c else 0), c, dt
 
 
@@ -594,6 +603,7 @@ def _matrix(K, dtype, device):
         raise ValueError("K is on %s, the inputs on %s" % (K.device, device))
     if not K.is_contiguous():
         raise ValueError("K must be contiguous")
+    _width(*shape)
     return shape
 
 
@@ -767,6 +777,7 @@ def orthogonalize(U, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
     batch = shape[0] if len(shape) % 2 else 1
     cols = shape[-1]
     rows = U.numel() // (batch * cols) if batch * cols else 0
+    _width(batch, rows, cols)
     a, b, c = coefficients
     need = orthogonalize_workspace_bytes(batch, rows, cols, dt)
     O = _new(O, shape, U.dtype, U, "O")

@@ -1,18 +1,19 @@
 // bf16 matrix products of the layer operators (mec_product.h), on v_mfma_f32_32x32x16_bf16.
 //
-// A workgroup computes a tile of Y, 32*BM*WM x 32*BN*WN, from chunks of 64 of the reduction
-// in two stages of LDS: while one chunk's products run, the next is on its way. Operands are
-// staged as they are stored:
-//   stored along the reduction ([m][k], [n][k])  rows of 64 k, 128 bytes; granule g (8 k) of
-//     row r at g ^ (r & 7); a fragment (8 k of one row per lane) is one 16-byte read
+// A workgroup computes a tile of Y, 32*BM*WM x 32*BN*WN, from chunks of KT (64 or 32) of the
+// reduction in stages of LDS: while one chunk's products run, the next (of 4 stages: the next
+// three) are on their way. Operands are staged as they are stored:
+//   stored along the reduction ([m][k], [n][k])  rows of KT k; granule g (8 k) of row r at
+//     g ^ (r & 7) (KT 32: g ^ (r / 2 & 3)); a fragment (8 k of one row per lane) is one
+//     16-byte read
 //   stored across it ([k][m], [k][n])  rows of one k; the 32-byte blocks (16 columns) of row
 //     k at block ^ (k & 7); a fragment is two transposing reads (ds_read_b64_tr_b16: 16
 //     lanes read 4 rows of 16 columns and each gets 4 k of one column)
 // Both orders put the lanes that read together on different banks. Rows of whole 16-byte
 // granules go straight to LDS (buffer_load .. lds; what lies past the end of the reduction
-// is past the resource's end and arrives as zeros); others go through registers, granules
-// cut off at the row's end element by element.
+// is past the resource's end and arrives as zeros); others go through registers.
 #include "mec_product.h"
+#include "mec_split.h"
 
 namespace mec {
 namespace {
@@ -33,12 +34,6 @@ struct Cfg {
     static_assert(TM * (KT / 8) % THREADS == 0 && TN * (KT / 8) % THREADS == 0 && LDS <= 160 * 1024, "tile");
     static_assert((kS - 2) * kLoads < 64, "loads in flight");
 };
-
-__device__ inline uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
-__device__ inline const char* scalar(const char* x) {
-    const uint64_t v = (uint64_t)x;
-    return (const char*)((uint64_t)scalar((uint32_t)(v >> 32)) << 32 | scalar((uint32_t)v));
-}
 
 // A raw buffer of `bytes` from `base` (both uniform), as the load's four scalar registers.
 __device__ inline u32x4v resource(const char* base, int64_t bytes) {
@@ -92,7 +87,7 @@ struct Operand {
         if constexpr (TR) {
             const int pos = tid % (T / 8), k = tid / (T / 8);
             const int col = (((pos >> 1) ^ (k & SW)) * 2 + (pos & 1)) * 8;
-            base = scalar(static_cast<const char*>(mem) + 2 * (k0 * ld + r0));
+            base = uniform(static_cast<const char*>(mem) + 2 * (k0 * ld + r0));
             step = 2 * KT * ld;
             have = count - r0 - col;
             k_at = k;
@@ -108,7 +103,7 @@ struct Operand {
             }
         } else {
             const int row = tid / G, kg = (tid % G) ^ swizzle(row);
-            base = scalar(static_cast<const char*>(mem) + 2 * (r0 * ld + k0));
+            base = uniform(static_cast<const char*>(mem) + 2 * (r0 * ld + k0));
             step = 2 * KT;
             left = k1 - k0;
             room = k1 >= 8;
@@ -194,7 +189,7 @@ __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
     using OpA = Operand<C::TM, C::THREADS, C::kKT, C::kAT, C::kDMA>;
     using OpB = Operand<C::TN, C::THREADS, C::kKT, C::kBT, C::kDMA>;
     __shared__ __align__(16) char lds[C::LDS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = (int)scalar((uint32_t)tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform((uint32_t)tid >> 6);
     const int wm = wave % C::kWM, wn = wave / C::kWM;
     const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
@@ -337,7 +332,7 @@ hipError_t run(Product p, hipStream_t stream) {
     if (p.clean) {
         hipLaunchKernelGGL(product_bf16_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
     } else {
-        using G = Cfg<BM, BN, WM, WN, KT, S, L, false>;
+        using G = Cfg<BM, BN, WM, WN, KT, 2, L, false>;
         hipLaunchKernelGGL(product_bf16_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
     }
     return hipGetLastError();

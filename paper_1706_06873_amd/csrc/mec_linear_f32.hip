@@ -253,7 +253,7 @@ hipError_t run(Product p, hipStream_t stream) {
     using C = Cfg<BM, BN, WM, WN, L, false>;
     p.m_tiles = (p.M + C::TM - 1) / C::TM;
     p.n_tiles = (p.N + C::TN - 1) / C::TN;
-    // shares are whole multiples of 64 elements, as product_splits counts them
+    // shares are whole multiples of 64 elements, as plan_product counts them
     const int64_t chunks = 2 * (((int64_t)p.K + 63) / 64);
     p.chunks = 2 * (int32_t)((chunks / 2 + p.splits - 1) / p.splits);
     const int64_t tiles = p.symmetric ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles;

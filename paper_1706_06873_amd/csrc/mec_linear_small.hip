@@ -296,7 +296,7 @@ uint32_t prepare(Product& p, Layout layout, int dtype) {
         p.clean = !(((uintptr_t)p.A | (uintptr_t)p.B) & 15u) && p.lda % 8 == 0 && p.ldb % 8 == 0 && a_run % 8 == 0 &&
                   b_run % 8 == 0 && p.a_batch % 8 == 0 && p.b_batch % 8 == 0;
     }
-    return blocks > 0x1fffff || p.splits > 1 ? 0 : (uint32_t)blocks;
+    return blocks > kMaxSmallBlocks || p.splits > 1 ? 0 : (uint32_t)blocks;
 }
 
 }  // namespace

@@ -38,8 +38,9 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 }  // namespace
 
 ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits, bool symmetric) {
-    const int64_t small_rounds = ceil_div(ceil_div(M, 32) * ceil_div(N, 32) * batch, 256);
-    ProductPlan best{0, 1, (double)small_rounds * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
+    const int64_t small = ceil_div(M, 32) * ceil_div(N, 32) * batch;
+    ProductPlan best{0, 1, (double)ceil_div(small, 256) * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
+    if (small > kMaxSmallBlocks) best.us = 1e30;
     const TileCost* const tiles = dtype ? kBf16 : kF32;
     const int count = dtype ? 5 : 3;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);

@@ -58,6 +58,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream);
 hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream);  // mec_linear.hip
 hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream);   // mec_linear_f32.hip
+constexpr int64_t kMaxSmallBlocks = 0x1fffff;  // of 1024 threads, in a launch
 hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream);  // mec_linear_small.hip
 // two small products, x of layout kXKt and k of kXtK, in one launch
 hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream);
@@ -443,7 +444,7 @@ __device__ inline void epilogue(const Product& p, const floatx16 (&acc)[BM][BN],
     }
 }
 
-// The mirror image of a wave's block of a symmetric Y (tile above the diagonal): register v
+// The mirror image of a wave's block of a symmetric Y (a tile below the diagonal): register v
 // of the 32 lanes with one n holds 32 consecutive m, a run of a row of the image.
 __device__ inline void mirror(const Product& p, const floatx16& acc, int32_t m0, int32_t n0, int32_t bat, int32_t split, int lane) {
     const int32_t m = m0 + (lane & 31);

@@ -523,6 +523,57 @@ def test_a_given_stream_owns_what_the_call_allocates():
         del busy
 
 
+def spread(t, pitch):
+    """t's rows `pitch` elements apart, in memory of their own."""
+    wide = torch.empty(t.shape[0], pitch, dtype=t.dtype, device=DEV)
+    wide[:, :t.shape[1]] = t.to(DEV)
+    return wide[:, :t.shape[1]]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,c,k_c", [(2100, 24, 40), (2305, 200, 264)])
+def test_rows_that_lie_past_32_bits(dtype, rows, c, k_c):
+    """The widest pitch: the last rows are more than 2^32 bytes (bf16) or elements' worth of
+    bytes on from the first. The same bits as from dense rows, which take the same kernels."""
+    g = torch.Generator().manual_seed(rows)
+    pitch = 1 << 20
+    X, R, K, G = randn(g, rows, c), randn(g, rows, k_c), randn(g, c, k_c) / 5, randn(g, rows, k_c)
+    X, R, K, G = (t.to(dtype).to(DEV) for t in (X, R, K, G))
+    print("[case]", dtype, rows, c, k_c, flush=True)
+    want = mec.linear(X, K, residual=R, act="relu")
+    Y = spread(torch.zeros(rows, k_c, dtype=dtype), pitch)
+    mec.linear(spread(X, pitch), K, residual=spread(R, pitch), act="relu", Y=Y)
+    assert torch.equal(Y, want)
+    Z = mec.linear(X, K)
+    want = mec.linear_grad(G, X, K, Z=Z, act="silu")
+    got = mec.linear_grad(spread(G, pitch), spread(X, pitch), K, Z=Z, act="silu")
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    want = mec.linear_grad(G, X, K, act="none")
+    got = mec.linear_grad(spread(G, pitch), spread(X, pitch), K, act="none")
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    want = mec.layer_norm(X)
+    Y = spread(torch.zeros(rows, c, dtype=dtype), pitch)
+    got = mec.layer_norm(spread(X, pitch), Y=Y)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    H = randn(g, rows, c).to(dtype).to(DEV)
+    want = mec.layer_norm_grad(H, X, *got[1:])
+    got = mec.layer_norm_grad(spread(H, pitch), spread(X, pitch), *got[1:])
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_stacks_past_32_bits():
+    """150 matrices of 7.6 million elements, 4.6 GB: the last comes out as it does alone."""
+    g = torch.Generator().manual_seed(31)
+    one = randn(g, 3811, 2000).to(DEV)
+    stack = torch.zeros(150, 3811, 2000, device=DEV)
+    stack[149] = one
+    stack[77, :, 5] = 1.0
+    got = mec.orthogonalize(stack, steps=2)
+    assert not got[0].any() and torch.isfinite(got[149]).all()
+    alone = mec.orthogonalize(one, steps=2)
+    assert (got[149] - alone).norm() <= 2.0 ** -16 * alone.norm()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_the_suites_block(capsys, dtype):
     import json

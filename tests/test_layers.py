@@ -189,6 +189,18 @@ def test_binding_refuses_updates():
         mec.orthogonalize(_t(0, 4))
 
 
+def test_binding_refuses_sizes_past_the_interfaces_int():
+    big = 1 << 32  # would arrive as 0, and 5 more as 5
+    meta = lambda *shape: torch.empty(shape, device="meta")
+    for call in (lambda: mec.linear(meta(2, big + 5), meta(big + 5, 4)), lambda: mec.linear(meta(2, 4), meta(4, big + 5)),
+                 lambda: mec.linear_grad(meta(2, big + 5), meta(2, 4), meta(4, big + 5)), lambda: mec.layer_norm(meta(2, big + 5)),
+                 lambda: mec.orthogonalize(meta(big + 5, 2)), lambda: mec.orthogonalize(meta(2, big + 5)),
+                 lambda: mec.orthogonalize(meta(big + 5, 2, 2))):
+        with pytest.raises(mec.MecError) as e:
+            call()
+        assert e.value.status == -5
+
+
 # ---------------------------------------------------------------- which kernel a product takes
 
 @pytest.mark.parametrize("layout,dtype,M,N,K,batch,split,want", [
