@@ -345,7 +345,7 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
  * or G's where g_pitch = k_c. Otherwise outputs must overlap neither each other nor
  * the inputs.
  * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for the partial sums of
- * dK and dbias; may be NULL where neither is wanted. */
+ * dK and dbias; may be NULL where that is 0 (few rows) or neither is wanted. */
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);
 int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX,
                     void* dK, float* dbias, void* workspace, size_t workspace_bytes, int64_t rows,

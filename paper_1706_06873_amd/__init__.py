@@ -500,11 +500,10 @@ def _pitch(t, name, c):
     raise ValueError("%s must be contiguous, or rows of contiguous channels" % name)
 
 
-def _width(*sizes):
+def _width(n):
     """Sizes past the C interface's int are refused here, the others there."""
-    for n in sizes:
-        if n > 0x7fffffff:
-            raise MecError(_UNSUPPORTED, "a size of %d" % n)
+    if n > 0x7fffffff:
+        raise MecError(_UNSUPPORTED, "a size of %d" % n)
 
 
 def _channels(t, name):
@@ -520,13 +519,15 @@ def _channels(t, name):
     return shape, (t.numel() // c if c else 0), c, dt
 
 
-def _ptr(t, name):
-    """The device pointer of a checked tensor, or None."""
-    if t is None:
-        return None
+def _on_device(t, name):
+    """Refuses a tensor in host memory; the others are where this one is."""
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    return t.data_ptr()
+
+
+def _ptr(t):
+    """The pointer of a checked tensor, or None."""
+    return None if t is None else t.data_ptr()
 
 
 def _dense(t, shape, dtype, device, name):
@@ -579,7 +580,7 @@ def _on(stream, call, ref, *args, **kwargs):
 def _scratch(need, workspace, ref):
     """(workspace, bytes): a given one is checked for size and device, else one is made."""
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=ref.device), need
+        return (ref.new_empty(need, dtype=torch.uint8) if need else None), need
     nbytes = workspace.numel() * workspace.element_size()
     if workspace.device != ref.device:
         raise ValueError("workspace is on %s, the inputs on %s" % (workspace.device, ref.device))
@@ -603,7 +604,7 @@ def _matrix(K, dtype, device):
         raise ValueError("K is on %s, the inputs on %s" % (K.device, device))
     if not K.is_contiguous():
         raise ValueError("K must be contiguous")
-    _width(*shape)
+    _width(shape[1])
     return shape
 
 
@@ -639,8 +640,9 @@ def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=N
         y_pitch = _activations(Y, "Y", k_c, dtype, device)
     if Z is not None:
         _dense(Z, shape, dtype, device, "Z")
-    _launch("mec_linear", device, _ptr(X, "X"), _ptr(K, "K"), _ptr(bias, "bias"), _ptr(residual, "residual"),
-            _ptr(Y, "Y"), _ptr(Z, "Z"), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0)
+    _on_device(X, "X")
+    _launch("mec_linear", device, X.data_ptr(), K.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(),
+            _ptr(Z), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0)
     return Y
 
 
@@ -686,9 +688,9 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     nbytes = 0
     if need_k or need_b:
         workspace, nbytes = _scratch(linear_grad_workspace_bytes(rows, i_c, k_c, dt), workspace, G)
-    _launch("mec_linear_grad", device, _ptr(G, "G"), _ptr(X, "X"), _ptr(K, "K"), _ptr(Z, "Z"),
-            _ptr(dZ, "dZ") if a else None, _ptr(dX, "dX"), _ptr(dK, "dK"), _ptr(dbias, "dbias"),
-            _ptr(workspace, "workspace") if nbytes else None, nbytes, rows, i_c, k_c, g_pitch, x_pitch, dt, a)
+    _on_device(G, "G")
+    _launch("mec_linear_grad", device, G.data_ptr(), _ptr(X), K.data_ptr(), _ptr(Z), _ptr(dZ) if a else None, _ptr(dX),
+            _ptr(dK), _ptr(dbias), _ptr(workspace) if nbytes else None, nbytes, rows, i_c, k_c, g_pitch, x_pitch, dt, a)
     return dX, dK, dbias, dZ
 
 
@@ -714,8 +716,9 @@ def layer_norm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None,
         y_pitch = _activations(Y, "Y", c, X.dtype, device)
     mean = _new(mean, pixels, _F32, X, "mean")
     rstd = _new(rstd, pixels, _F32, X, "rstd")
-    _launch("mec_layer_norm", device, _ptr(X, "X"), _ptr(gamma, "gamma"), _ptr(beta, "beta"), _ptr(Y, "Y"),
-            _ptr(mean, "mean"), _ptr(rstd, "rstd"), rows, c, x_pitch, y_pitch, eps, dt)
+    _on_device(X, "X")
+    _launch("mec_layer_norm", device, X.data_ptr(), _ptr(gamma), _ptr(beta), Y.data_ptr(), mean.data_ptr(),
+            rstd.data_ptr(), rows, c, x_pitch, y_pitch, eps, dt)
     return Y, mean, rstd
 
 
@@ -747,9 +750,9 @@ def layer_norm_grad(G, X, mean, rstd, gamma=None, needs=(True, True, True), dX=N
     nbytes = 0
     if needs[1] or needs[2]:
         workspace, nbytes = _scratch(layer_norm_grad_workspace_bytes(rows, c, dt), workspace, X)
-    _launch("mec_layer_norm_grad", device, _ptr(G, "G"), _ptr(X, "X"), _ptr(gamma, "gamma"), _ptr(mean, "mean"),
-            _ptr(rstd, "rstd"), _ptr(dX, "dX"), _ptr(dgamma, "dgamma"), _ptr(dbeta, "dbeta"),
-            _ptr(workspace, "workspace") if nbytes else None, nbytes, rows, c, g_pitch, x_pitch, dt)
+    _on_device(X, "X")
+    _launch("mec_layer_norm_grad", device, G.data_ptr(), X.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(),
+            _ptr(dX), _ptr(dgamma), _ptr(dbeta), _ptr(workspace) if nbytes else None, nbytes, rows, c, g_pitch, x_pitch, dt)
     return dX, dgamma, dbeta
 
 
@@ -777,11 +780,13 @@ def orthogonalize(U, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
     batch = shape[0] if len(shape) % 2 else 1
     cols = shape[-1]
     rows = U.numel() // (batch * cols) if batch * cols else 0
-    _width(batch, rows, cols)
+    for n in (batch, rows, cols):
+        _width(n)
     a, b, c = coefficients
     need = orthogonalize_workspace_bytes(batch, rows, cols, dt)
     O = _new(O, shape, U.dtype, U, "O")
     workspace, nbytes = _scratch(need, workspace, U)
-    _launch("mec_orthogonalize", U.device, _ptr(U, "U"), _ptr(O, "O"), _ptr(workspace, "workspace"), nbytes,
+    _on_device(U, "U")
+    _launch("mec_orthogonalize", U.device, U.data_ptr(), O.data_ptr(), workspace.data_ptr(), nbytes,
             batch, rows, cols, steps, a, b, c, eps, dt)
     return O

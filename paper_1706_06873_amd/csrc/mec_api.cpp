@@ -343,7 +343,8 @@ bool valid_act(int act) { return act >= MEC_ACT_NONE && act <= MEC_ACT_GELU; }
 
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
     const int64_t s = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, 64).splits;
-    const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = mec::act_grad_shares(rows, k_c) * k_c * 4;
+    const int64_t shares = mec::act_grad_shares(rows, k_c);  // one share goes straight to dbias
+    const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = shares > 1 ? shares * k_c * 4 : 0;
     return dk > db ? dk : db;
 }
 
@@ -399,8 +400,10 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     if (!aligned(G, es) || !aligned(X, es) || !aligned(K, es) || !aligned(Z, es) || !aligned(dZ, es) || !aligned(dX, es) ||
         !aligned(dK, es) || !aligned(dbias, 4))
         return MEC_ERR_ALIGNMENT;
-    if ((dK || dbias) && (!workspace || (uint64_t)workspace_bytes < (uint64_t)linear_grad_bytes(rows, i_c, k_c, dtype)))
-        return MEC_ERR_WORKSPACE;
+    if (dK || dbias) {
+        const int64_t need = linear_grad_bytes(rows, i_c, k_c, dtype);
+        if (need && (!workspace || (uint64_t)workspace_bytes < (uint64_t)need)) return MEC_ERR_WORKSPACE;
+    }
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     const hipStream_t st = (hipStream_t)stream;
     float* const part = static_cast<float*>(workspace);

@@ -82,9 +82,9 @@ def test_alignment_of_16_bits():
 
 
 def test_workspaces():
-    need = mec.linear_grad_workspace_bytes(7, 5, 6)
-    assert need > 0
-    assert linear_grad(wb=need - 1) == -2 and linear_grad(ws=NULL) == -2
+    need = mec.linear_grad_workspace_bytes(700, 5, 6)
+    assert need > 0 and mec.linear_grad_workspace_bytes(7, 5, 6) == 0  # few rows need none
+    assert linear_grad(rows=700, wb=need - 1) == -2 and linear_grad(rows=700, ws=NULL) == -2
     need = mec.layer_norm_grad_workspace_bytes(7, 5)
     assert need > 0
     assert norm_grad(wb=need - 1) == -2 and norm_grad(ws=NULL) == -2
@@ -145,7 +145,7 @@ def test_binding_refuses_linear_gradients():
         (dict(act="relu", Z=Z.bfloat16()), ValueError, "Z must be"),
         (dict(act="silu", Z=Z, dZ=_t(7, 6)), ValueError, "dZ must be"), (dict(dX=_t(8, 6)), ValueError, "dX must be"),
         (dict(dK=_t(6, 5)), ValueError, "dK must be"), (dict(dbias=_t(5)), ValueError, "dbias must be"),
-        (dict(workspace=_t(1, dtype=torch.uint8)), ValueError, "workspace holds"),
+        (dict(G=_t(300, 6), X=_t(300, 5), workspace=_t(1, dtype=torch.uint8)), ValueError, "workspace holds"),
         (dict(needs=(True, False, False)), ValueError, "device tensor"),
     ]:
         with pytest.raises(error, match=match):
