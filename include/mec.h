@@ -330,10 +330,14 @@ enum mec_act { MEC_ACT_NONE = 0, MEC_ACT_RELU = 1, MEC_ACT_SILU = 2, MEC_ACT_GEL
  * NULL. Z, unless NULL, receives z (rows x k_c, dense, rounded to dtype) for the
  * backward pass. R may be Y itself (then r_pitch = y_pitch); otherwise Y and Z
  * must not overlap each other or the inputs.
+ * workspace: mec_linear_workspace_bytes, 4-byte aligned, for the partial sums of a product
+ * whose few outputs leave compute units idle; may be NULL where that is 0.
  * Returns MEC_OK or a negative status. */
+int64_t mec_linear_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);
 int mec_linear(const void* X, const void* K, const float* bias, const void* R, void* Y, void* Z,
                int64_t rows, int i_c, int k_c, int64_t x_pitch, int64_t r_pitch, int64_t y_pitch,
-               int dtype, int act, int residual_first, void* stream);
+               int dtype, int act, int residual_first, void* workspace, size_t workspace_bytes,
+               void* stream);
 
 /* Its gradients, for G = dloss/dY (rows x k_c):
  *   dZ = G act'(Z),  dX = dZ K^T,  dK = X^T dZ,  dbias = column sums of dZ
@@ -344,8 +348,8 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
  * always written, and products take it as rounded to dtype; it may be Z's memory,
  * or G's where g_pitch = k_c. Otherwise outputs must overlap neither each other nor
  * the inputs.
- * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for the partial sums of
- * dK and dbias; may be NULL where that is 0 (few rows) or neither is wanted. */
+ * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for partial sums; may be NULL
+ * where that is 0 or none of dX, dK and dbias is wanted. */
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);
 int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX,
                     void* dK, float* dbias, void* workspace, size_t workspace_bytes, int64_t rows,

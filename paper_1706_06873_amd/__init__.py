@@ -12,6 +12,7 @@ Layouts (paper notation): I is i_n x i_h x i_w x i_c, K is k_h x k_w x i_c x
 k_c, O is i_n x o_h x o_w x k_c (fp32). I and K are both fp32 or both bf16.
 """
 import ctypes
+import functools
 import os
 
 # torch first: importing it loads its HIP runtime, and libmec.so then binds to
@@ -26,7 +27,7 @@ __all__ = [
     "GRAD_INPUT", "GRAD_KERNEL", "GRAD_KERNEL_FROM_L", "grad_workspace_bytes", "fold",
     "dgrad_gemm", "conv2d_dgrad", "wgrad_gemm", "conv2d_wgrad", "noalloc_scratch_bytes",
     "conv2d_wgrad_noalloc",
-    "linear", "linear_grad", "linear_grad_workspace_bytes", "layer_norm", "layer_norm_grad",
+    "linear", "linear_workspace_bytes", "linear_grad", "linear_grad_workspace_bytes", "layer_norm", "layer_norm_grad",
     "layer_norm_grad_workspace_bytes", "orthogonalize", "orthogonalize_workspace_bytes",
 ]
 
@@ -79,7 +80,8 @@ def _load(path):
     L.mec_conv2d_wgrad_noalloc.argtypes = [_vp, _vp, _vp] + _DIMS + [_i, _vp]
     L.mec_conv2d_wgrad_noalloc.restype = _i
     i64, sz, f = ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
-    L.mec_linear.argtypes = [_vp] * 6 + [i64, _i, _i, i64, i64, i64, _i, _i, _i, _vp]
+    L.mec_linear.argtypes = [_vp] * 6 + [i64, _i, _i, i64, i64, i64, _i, _i, _i, _vp, sz, _vp]
+    L.mec_linear_workspace_bytes.argtypes = [i64, _i, _i, _i]
     L.mec_linear_grad_workspace_bytes.argtypes = [i64, _i, _i, _i]
     L.mec_linear_grad.argtypes = [_vp] * 9 + [sz, i64, _i, _i, i64, i64, _i, _i, _vp]
     L.mec_layer_norm.argtypes = [_vp] * 6 + [i64, _i, i64, i64, f, _i, _vp]
@@ -89,7 +91,7 @@ def _load(path):
     L.mec_orthogonalize.argtypes = [_vp] * 3 + [sz, _i, _i, _i, _i, f, f, f, f, _i, _vp]
     for name in ("linear", "linear_grad", "layer_norm", "layer_norm_grad", "orthogonalize"):
         getattr(L, "mec_" + name).restype = _i
-        if name not in ("linear", "layer_norm"):
+        if name != "layer_norm":
             getattr(L, "mec_%s_workspace_bytes" % name).restype = i64
     L.mec_strerror.argtypes = [_i]
     L.mec_strerror.restype = ctypes.c_char_p
@@ -473,7 +475,8 @@ def conv2d_wgrad_noalloc(I, G, k_h, k_w, s_h=1, s_w=1, dK=None, stream=None):
 # Activations are tensors with the channels last: contiguous, or 2-D (rows x channels) with
 # a row pitch, as a slice of a wider tensor's channels has. They, their gradients, K and dK
 # are float32 or bfloat16, all the same; bias, gamma, beta, their gradients and the row
-# statistics are float32.
+# statistics are float32. The *_workspace_bytes functions are functions of the sizes alone and
+# remember their values (0.5 us of a call).
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _F32 = torch.float32
@@ -608,13 +611,15 @@ def _matrix(K, dtype, device):
     return shape
 
 
-def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=None, Z=None, stream=None):
+def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=None, Z=None, workspace=None,
+           stream=None):
     """Y = act(X K + bias) + residual, or act(X K + bias + residual) with residual_first, for
     every pixel of X (... x i_c) and K of i_c x k_c (or 1 x 1 x i_c x k_c); act is "none",
     "relu", "silu" or "gelu" (the tanh form). A given Z (Y's shape) receives act's argument,
-    for linear_grad. residual may be Y itself. Returns Y."""
+    for linear_grad. residual may be Y itself. A given workspace holds at least
+    linear_workspace_bytes bytes. Returns Y."""
     if stream is not None:
-        return _on(stream, linear, X, K, bias, residual, act, residual_first, Y, Z)
+        return _on(stream, linear, X, K, bias, residual, act, residual_first, Y, Z, workspace)
     xs, rows, i_c, dt = _channels(X, "X")
     device, dtype = X.device, X.dtype
     ki, k_c = _matrix(K, dtype, device)
@@ -640,12 +645,20 @@ def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=N
         y_pitch = _activations(Y, "Y", k_c, dtype, device)
     if Z is not None:
         _dense(Z, shape, dtype, device, "Z")
+    workspace, nbytes = _scratch(linear_workspace_bytes(rows, i_c, k_c, dt), workspace, X)
     _on_device(X, "X")
     _launch("mec_linear", device, X.data_ptr(), K.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(),
-            _ptr(Z), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0)
+            _ptr(Z), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0,
+            _ptr(workspace) if nbytes else None, nbytes)
     return Y
 
 
+@functools.lru_cache(4096)
+def linear_workspace_bytes(rows, i_c, k_c, dtype=F32):
+    return _check(lib.mec_linear_workspace_bytes(rows, i_c, k_c, dtype), "mec_linear_workspace_bytes")
+
+
+@functools.lru_cache(4096)
 def linear_grad_workspace_bytes(rows, i_c, k_c, dtype=F32):
     return _check(lib.mec_linear_grad_workspace_bytes(rows, i_c, k_c, dtype), "mec_linear_grad_workspace_bytes")
 
@@ -686,7 +699,7 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     dK = _new(dK, K.shape, dtype, G, "dK") if need_k else None
     dbias = _new(dbias, (k_c,), _F32, G, "dbias") if need_b else None
     nbytes = 0
-    if need_k or need_b:
+    if need_x or need_k or need_b:
         workspace, nbytes = _scratch(linear_grad_workspace_bytes(rows, i_c, k_c, dt), workspace, G)
     _on_device(G, "G")
     _launch("mec_linear_grad", device, G.data_ptr(), _ptr(X), K.data_ptr(), _ptr(Z), _ptr(dZ) if a else None, _ptr(dX),
@@ -722,6 +735,7 @@ def layer_norm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None,
     return Y, mean, rstd
 
 
+@functools.lru_cache(4096)
 def layer_norm_grad_workspace_bytes(rows, channels, dtype=F32):
     return _check(lib.mec_layer_norm_grad_workspace_bytes(rows, channels, dtype),
                   "mec_layer_norm_grad_workspace_bytes")
@@ -756,6 +770,7 @@ def layer_norm_grad(G, X, mean, rstd, gamma=None, needs=(True, True, True), dX=N
     return dX, dgamma, dbeta
 
 
+@functools.lru_cache(4096)
 def orthogonalize_workspace_bytes(batch, rows, cols, dtype=F32):
     return _check(lib.mec_orthogonalize_workspace_bytes(batch, rows, cols, dtype),
                   "mec_orthogonalize_workspace_bytes")

@@ -6,6 +6,7 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <initializer_list>
 
 #include "mec_internal.h"
@@ -339,20 +340,36 @@ int first_error(std::initializer_list<int> codes) {
     return MEC_OK;
 }
 
+// A product by its plan, the shares of its reduction (in p.part) added up; without an
+// epilogue of its own Y is dense.
+hipError_t launch_shared(const mec::ProductPlan& plan, mec::Layout layout, mec::Product p, int dtype, hipStream_t stream) {
+    const hipError_t e = mec::launch_product(plan, layout, p, dtype, stream);
+    if (e != hipSuccess || plan.splits == 1) return e;
+    if (layout != mec::Layout::kXK) return mec::launch_sum_parts(p.part, plan.splits, (int64_t)p.M * p.N, p.Y, dtype, stream);
+    p.splits = plan.splits;
+    return mec::launch_finish_parts(p, dtype, stream);
+}
+
 bool valid_act(int act) { return act >= MEC_ACT_NONE && act <= MEC_ACT_GELU; }
 
+constexpr int32_t kMaxShares = 64;  // of a product's reduction
+
+// the sums of a product's shares
+int64_t parts_bytes(const mec::ProductPlan& plan, int64_t M, int64_t N) { return plan.splits > 1 ? plan.splits * M * N * 4 : 0; }
+
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
-    const int64_t s = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, 64).splits;
+    const int64_t dx = parts_bytes(mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares), rows, i_c);
+    const int64_t dk = parts_bytes(mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares), i_c, k_c);
     const int64_t shares = mec::act_grad_shares(rows, k_c);  // one share goes straight to dbias
-    const int64_t dk = s > 1 ? s * i_c * k_c * 4 : 0, db = shares > 1 ? shares * k_c * 4 : 0;
-    return dk > db ? dk : db;
+    const int64_t db = shares > 1 ? shares * k_c * 4 : 0;
+    return std::max({dx, dk, db});
 }
 
 }  // namespace
 
 int mec_linear(const void* X, const void* K, const float* bias, const void* R, void* Y, void* Z, int64_t rows, int i_c,
                int k_c, int64_t x_pitch, int64_t r_pitch, int64_t y_pitch, int dtype, int act, int residual_first,
-               void* stream) {
+               void* workspace, size_t workspace_bytes, void* stream) {
     const int rc = first_error({check_rows(rows, i_c, x_pitch), check_rows(rows, k_c, y_pitch),
                                 R ? check_rows(rows, k_c, r_pitch) : MEC_OK});
     if (rc != MEC_OK) return rc;
@@ -360,6 +377,11 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     const int64_t es = elem_bytes(dtype);
     if (!aligned(X, es) || !aligned(K, es) || !aligned(bias, 4) || !aligned(R, es) || !aligned(Y, es) || !aligned(Z, es))
         return MEC_ERR_ALIGNMENT;
+    const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares);
+    if (plan.splits > 1 &&
+        (!workspace || (uint64_t)workspace_bytes < (uint64_t)parts_bytes(plan, rows, k_c)))
+        return MEC_ERR_WORKSPACE;
+    if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     mec::Product p{};
     p.A = X;
     p.B = K;
@@ -377,9 +399,17 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     p.act = act;
     p.res_first = residual_first != 0;
     p.alpha = p.beta = 1.0f;
-    p.splits = p.batch = 1;
+    p.batch = 1;
+    p.part = static_cast<float*>(workspace);
     clear_stale_error();
-    return hip_status(mec::launch_product(mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
+    return hip_status(launch_shared(plan, mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
+}
+
+int64_t mec_linear_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
+    const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
+    return parts_bytes(mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares), rows, k_c);
 }
 
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
@@ -400,7 +430,7 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     if (!aligned(G, es) || !aligned(X, es) || !aligned(K, es) || !aligned(Z, es) || !aligned(dZ, es) || !aligned(dX, es) ||
         !aligned(dK, es) || !aligned(dbias, 4))
         return MEC_ERR_ALIGNMENT;
-    if (dK || dbias) {
+    if (dX || dK || dbias) {
         const int64_t need = linear_grad_bytes(rows, i_c, k_c, dtype);
         if (need && (!workspace || (uint64_t)workspace_bytes < (uint64_t)need)) return MEC_ERR_WORKSPACE;
     }
@@ -437,20 +467,16 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     k.N = k_c;
     k.K = (int32_t)rows;
     k.part = part;
-    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x.M, x.N, x.K, 1, 1);
-    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k.M, k.N, k.K, 1, 64);
+    x.part = part;
+    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x.M, x.N, x.K, 1, kMaxShares);
+    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k.M, k.N, k.K, 1, kMaxShares);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
     if (dX) {
-        rc = hip_status(mec::launch_product(px, mec::Layout::kXKt, x, dtype, st), "gradient of the input");
+        rc = hip_status(launch_shared(px, mec::Layout::kXKt, x, dtype, st), "gradient of the input");
         if (rc != MEC_OK) return rc;
     }
-    if (dK) {
-        rc = hip_status(mec::launch_product(pk, mec::Layout::kXtK, k, dtype, st), "gradient of the kernel");
-        if (rc == MEC_OK && pk.splits > 1)
-            rc = hip_status(mec::launch_sum_parts(part, pk.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
-    }
-    return rc;
+    return dK ? hip_status(launch_shared(pk, mec::Layout::kXtK, k, dtype, st), "gradient of the kernel") : MEC_OK;
 }
 
 int mec_layer_norm(const void* X, const float* gamma, const float* beta, void* Y, float* mean, float* rstd, int64_t rows,
@@ -585,7 +611,7 @@ int mec_internal_wgrad(int kernel, const void* A, const float* G, float* dK, voi
 }
 
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
-    const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? 64 : 1);
+    const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? kMaxShares : 1);
     return p.kernel + 16 * p.splits;
 }
 

@@ -142,6 +142,74 @@ hipError_t sum_parts(const float* part, int64_t count, int64_t n, int64_t n0, vo
     return hipGetLastError();
 }
 
+// What a product's epilogue does, for one whose reduction was shared: 8 columns of a row per
+// thread, then bias, activation and residual. WAYS threads add every WAYS-th share each, and
+// the first of them joins the sums in order.
+template <class E, int WAYS>
+__global__ __launch_bounds__(256) void finish_parts_kernel(Product p, uint32_t granules, uint32_t count) {
+    constexpr bool FAST = sizeof(E) == 2;
+    constexpr uint32_t PER = 256 / WAYS;
+    __shared__ __align__(16) float sums[WAYS > 1 ? 256 * 8 : 1];
+    const uint32_t at = threadIdx.x % PER, way = threadIdx.x / PER;
+    const int64_t stride = (int64_t)p.M * p.N;
+    for (uint32_t first = blockIdx.x * PER; first < count; first += gridDim.x * PER) {
+        const uint32_t i = first + at < count ? first + at : count - 1;
+        const int64_t m = i / granules;
+        const int32_t n = (int32_t)(i - (uint32_t)m * granules) * 8, have = p.N - n;
+        Pack8<E> r;
+        if (p.R && way == 0) r.load(static_cast<const E*>(p.R) + m * p.ldr + n, have);
+        const float* const part = p.part + m * p.N + n;
+        float v[8] = {};
+#pragma unroll 4
+        for (int32_t s = (int32_t)way; s < p.splits; s += WAYS) {
+            Pack8<float> w;
+            w.load(part + s * stride, have);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += e < have ? w.get(e) : 0.0f;
+        }
+        if constexpr (WAYS > 1) {
+            __syncthreads();
+            store8v(sums + threadIdx.x * 8, v);
+            __syncthreads();
+            if (way == 0)
+#pragma unroll
+                for (int w = 1; w < WAYS; ++w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += sums[(w * PER + at) * 8 + e];
+        }
+        if (way || first + at >= count) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] *= p.alpha;
+            if (p.bias && e < have) v[e] += p.bias[n + e];
+            if (p.R && p.res_first) v[e] += p.beta * r.get(e);
+        }
+        Pack8<E> o;
+        if (p.Z) {
+            o.round(v);
+            o.store(static_cast<E*>(p.Z) + m * p.ldz + n, have);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (p.act == kActRelu) v[e] = act_value<FAST>(kActRelu, v[e]);
+            else if (p.act == kActSilu) v[e] = act_value<FAST>(kActSilu, v[e]);
+            else if (p.act == kActGelu) v[e] = act_value<FAST>(kActGelu, v[e]);
+            if (p.R && !p.res_first) v[e] += p.beta * r.get(e);
+        }
+        o.round(v);
+        o.store(static_cast<E*>(p.Y) + m * p.ldy + n, have);
+    }
+}
+template <class E, int WAYS>
+hipError_t finish_parts(const Product& p, hipStream_t stream) {
+    const int64_t granules = (p.N + 7) / 8, count = granules * p.M;
+    if (count > 0x7fffffff || p.batch != 1) return hipErrorInvalidValue;
+    const int64_t blocks = (count * WAYS + 255) / 256;
+    hipLaunchKernelGGL((finish_parts_kernel<E, WAYS>), dim3((uint32_t)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream, p,
+                       (uint32_t)granules, (uint32_t)count);
+    return hipGetLastError();
+}
+
 template <class E, int TX, int THREADS>
 hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream) {
     const uint32_t strips = (uint32_t)((p.N + 8 * TX - 1) / (8 * TX));
@@ -161,6 +229,10 @@ hipError_t act_grad(const ActGradParams& p, uint32_t shares, hipStream_t stream)
 
 }  // namespace
 
+hipError_t launch_finish_parts(const Product& p, int dtype, hipStream_t stream) {
+    if (p.splits > 6) return dtype ? finish_parts<uint16_t, 8>(p, stream) : finish_parts<float, 8>(p, stream);
+    return dtype ? finish_parts<uint16_t, 1>(p, stream) : finish_parts<float, 1>(p, stream);
+}
 hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* out, int dtype, hipStream_t stream) {
     return dtype ? sum_parts<uint16_t>(part, count, n, n, out, nullptr, stream)
                  : sum_parts<float>(part, count, n, n, out, nullptr, stream);

@@ -147,7 +147,8 @@ constexpr int kRun = 64;                  // k per turn: 4 fragments of each ope
 constexpr int kPatch = kRun * 32 * 2;     // bytes of a wave's patch: 64 rows of 32 columns
 
 // The 4 fragments of an operand for the 64 k from k on, in two parts: loads, and what makes
-// fragments of them. CLEAN: 16-byte rows of whole granules.
+// fragments of them. CLEAN: 16-byte rows of whole granules; else granules are read whole at
+// any boundary, but for those that the row or the reduction cuts off.
 template <bool TR, bool CLEAN>
 struct Turn {
     u32x4v w[4];
@@ -161,6 +162,9 @@ struct Turn {
                 if constexpr (CLEAN) {
                     w[i] = *reinterpret_cast<const u32x4v*>(src + (c < r ? c : r - 8));
                     if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
+                } else if (r >= 32) {  // (uniform)
+                    w[i] = load_any(src + c);
+                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
                 } else {
                     w[i] = load_some(src + c, at < k1 ? r - c : 0);
                 }
@@ -169,6 +173,9 @@ struct Turn {
                 const uint16_t* const src = base + ((lane & 31) < r ? (lane & 31) : r - 1) * ld;
                 if constexpr (CLEAN) {
                     w[i] = *reinterpret_cast<const u32x4v*>(src + (at < k1 ? at : k1 - 8));
+                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
+                } else if (k1 % 8 == 0) {  // (uniform)
+                    w[i] = load_any(src + (at < k1 ? at : k1 - 8));
                     if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
                 } else {
                     w[i] = load_some(src + at, k1 - at);

@@ -37,13 +37,27 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 
 }  // namespace
 
-ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits, bool symmetric) {
-    const int64_t small = ceil_div(M, 32) * ceil_div(N, 32) * batch;
-    ProductPlan best{0, 1, (double)ceil_div(small, 256) * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K)};
-    if (small > kMaxSmallBlocks) best.us = 1e30;
+ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
+                         bool symmetric) {
     const TileCost* const tiles = dtype ? kBf16 : kF32;
     const int count = dtype ? 5 : 3;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
+    // A call of one product in shares takes its caller's thread a second launch and a workspace
+    // (13 us, so 8; 1 x 2048 x 1000 in bf16 in one launch 7.5 us, in shares 14.0): below that
+    // the GPU's time is not what counts. Where other launches stand around it anyway
+    // (dK, a symmetric product) it is.
+    const bool alone = layout != Layout::kXtK && !symmetric;
+    ProductPlan best{0, 1, 1e30};
+    double least = 1e30;
+    auto offer = [&](int32_t kernel, int64_t splits, double us) {
+        const double host = !alone ? 0.0 : splits > 1 ? 13.0 : 8.0, t = us > host ? us : host;
+        if (t < least || (t == least && us < best.us)) {
+            least = t;
+            best = {kernel, (int32_t)splits, us};
+        }
+    };
+    const int64_t small = ceil_div(M, 32) * ceil_div(N, 32) * batch;
+    if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K));
     for (int i = 0; i < count; ++i) {
         int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn);
         if (symmetric && !dtype && i + 1 == kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
@@ -53,8 +67,8 @@ ProductPlan plan_product(Layout, int dtype, int64_t M, int64_t N, int64_t K, int
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
-            if (real > 1) us += 3.0 + (double)(real * batch * M * N) / 8e5;  // the sum of the shares
-            if (us < best.us) best = {i + 1, (int32_t)real, us};
+            if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((real + (alone ? 1 : 0)) * batch * M * N) / 8e5;  // the sum of the shares
+            offer(i + 1, real, us);
         }
     }
     return best;

@@ -65,6 +65,8 @@ hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_
 // by the plan, in one share
 hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream);
 
+// Y, Z of a product (one, not a batch) from the sums of its shares in p.part
+hipError_t launch_finish_parts(const Product& p, int dtype, hipStream_t stream);
 // out[j] = sum over i < count of part[i*n + j], in a fixed order; out fp32 or bf16
 hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* out, int dtype, hipStream_t stream);
 // the same for 2 n columns, the first n to out and the others to out2 (either may be nullptr)

@@ -130,6 +130,32 @@ def test_linear_grad(dtype, rows, i_c, k_c):
         close(dK, want, ek + HALF[dtype] * (want.abs() + ek), "dK")
 
 
+LONG = [(70, 16384, 33), (512, 9000, 64), (1000, 4099, 131), (257, 8192, 72)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,i_c,k_c", LONG)
+def test_long_reductions_in_shares(dtype, rows, i_c, k_c):
+    """Few outputs of long reductions: the shares' sums lie in the workspace before the epilogue."""
+    code = mec.F32 if dtype is F32 else mec.BF16
+    if i_c > 8000 or dtype is F32:  # (in bf16 the shortest is not worth the second launch)
+        assert mec.linear_workspace_bytes(rows, i_c, k_c, code) >= 2 * rows * k_c * 4
+        assert mec.linear_grad_workspace_bytes(rows, k_c, i_c, code) >= 2 * rows * k_c * 4
+    test_linear(dtype, rows, i_c, k_c)
+    test_linear_grad(dtype, rows, k_c, i_c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_shares_in_place_with_a_workspace_of_the_callers(dtype):
+    g = torch.Generator().manual_seed(12)
+    X, K, R = (randn(g, *s).to(dtype).to(DEV) for s in ((512, 9000), (9000, 64), (512, 64)))
+    need = mec.linear_workspace_bytes(512, 9000, 64, mec.F32 if dtype is F32 else mec.BF16)
+    ws = torch.full((need + 64,), 0x7f, dtype=torch.uint8, device=DEV)
+    want = mec.linear(X, K, residual=R, act="gelu")
+    got = mec.linear(X, K, residual=R, act="gelu", Y=R, workspace=ws[:need])
+    assert got is R and torch.equal(R, want) and (ws[need:] == 0x7f).all()
+
+
 def test_linear_grad_wants_only_some():
     g = torch.Generator().manual_seed(5)
     X, K, G = randn(g, 70, 24).to(DEV), randn(g, 24, 40).to(DEV), randn(g, 70, 40).to(DEV)

@@ -14,8 +14,9 @@ BIG = 1 << 40
 F32, BF16 = mec.F32, mec.BF16
 
 
-def linear(X=FAKE, K=FAKE, bias=FAKE, R=FAKE, Y=FAKE, Z=FAKE, rows=7, i_c=5, k_c=6, xp=5, rp=6, yp=6, dtype=F32, act=1):
-    return mec.lib.mec_linear(X, K, bias, R, Y, Z, rows, i_c, k_c, xp, rp, yp, dtype, act, 0, NULL)
+def linear(X=FAKE, K=FAKE, bias=FAKE, R=FAKE, Y=FAKE, Z=FAKE, rows=7, i_c=5, k_c=6, xp=5, rp=6, yp=6, dtype=F32, act=1,
+           ws=FAKE, wb=BIG):
+    return mec.lib.mec_linear(X, K, bias, R, Y, Z, rows, i_c, k_c, xp, rp, yp, dtype, act, 0, ws, wb, NULL)
 
 
 def linear_grad(G=FAKE, X=FAKE, K=FAKE, Z=FAKE, dZ=FAKE, dX=FAKE, dK=FAKE, db=FAKE, ws=FAKE, wb=BIG, rows=7, i_c=5, k_c=6,
@@ -66,7 +67,7 @@ def test_beyond_the_kernels_limits(call, kw):
 
 
 @pytest.mark.parametrize("call,names", [
-    (linear, "X K bias R Y Z"), (linear_grad, "G X K Z dZ dX dK db ws"), (norm, "X gamma beta Y mean rstd"),
+    (linear, "X K bias R Y Z ws"), (linear_grad, "G X K Z dZ dX dK db ws"), (norm, "X gamma beta Y mean rstd"),
     (norm_grad, "G X gamma mean rstd dX dg db ws"), (orth, "U O"),
 ])
 def test_alignment(call, names):
@@ -82,6 +83,12 @@ def test_alignment_of_16_bits():
 
 
 def test_workspaces():
+    assert mec.linear_workspace_bytes(7, 5, 6) == 0  # no partial sums of short reductions
+    long = dict(rows=512, i_c=16384, k_c=64, xp=16384, rp=64, yp=64)
+    need = mec.linear_workspace_bytes(512, 16384, 64)
+    assert need >= 2 * 512 * 64 * 4
+    assert linear(wb=need - 1, **long) == -2 and linear(ws=NULL, **long) == -2
+    assert linear(ws=ODD, **long) == -3
     need = mec.linear_grad_workspace_bytes(700, 5, 6)
     assert need > 0 and mec.linear_grad_workspace_bytes(7, 5, 6) == 0  # few rows need none
     assert linear_grad(rows=700, wb=need - 1) == -2 and linear_grad(rows=700, ws=NULL) == -2
