@@ -148,12 +148,29 @@ constexpr int kPatch = kRun * 32 * 2;     // bytes of a wave's patch: 64 rows of
 
 // The 4 fragments of an operand for the 64 k from k on, in two parts: loads, and what makes
 // fragments of them. CLEAN: 16-byte rows of whole granules; else granules are read whole at
-// any boundary, but for those that the row or the reduction cuts off.
+// any boundary, but for those that the row or the reduction cuts off. Rows along the
+// reduction at odd elements go dword by dword (whole loads of 64 rows that begin inside
+// a dword: 64 x 256 <- 3239 41.7 us, so 24.2; at even elements 14.7 and 24).
+// 16 bytes as the whole dwords around them (a dword of which one half is an element's is
+// never cut by the end of a page)
+__device__ inline u32x4v load_dwords(const uint16_t* src) {
+    struct __attribute__((packed, aligned(4))) Any {
+        u32x4v v;
+    };
+    const uintptr_t at = (uintptr_t)src;
+    const u32x4v w = reinterpret_cast<const Any*>(at & ~(uintptr_t)3)->v;
+    const uint32_t last = *reinterpret_cast<const uint32_t*>((at + 14) & ~(uintptr_t)3);
+    const uint32_t by = (uint32_t)(at & 2) * 8;
+    return u32x4v{__builtin_amdgcn_alignbit(w[1], w[0], by), __builtin_amdgcn_alignbit(w[2], w[1], by),
+                  __builtin_amdgcn_alignbit(w[3], w[2], by), __builtin_amdgcn_alignbit(last, w[3], by)};
+}
+
 template <bool TR, bool CLEAN>
 struct Turn {
     u32x4v w[4];
     // base: the tile's first row (column); r: rows (columns) there are from it on
     __device__ inline void load(const uint16_t* base, int64_t ld, int32_t r, int32_t k, int32_t k1, int lane) {
+        const bool whole = k1 % 8 == 0, odd = (((uint64_t)base >> 1 | (uint64_t)ld) & 1) != 0;  // uniform
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (TR) {  // row k + 16 i + lane / 4, granule lane % 4 of its 32 columns
@@ -171,15 +188,11 @@ struct Turn {
             } else {
                 const int32_t at = k + 16 * i + 8 * (lane >> 5);
                 const uint16_t* const src = base + ((lane & 31) < r ? (lane & 31) : r - 1) * ld;
-                if constexpr (CLEAN) {
-                    w[i] = *reinterpret_cast<const u32x4v*>(src + (at < k1 ? at : k1 - 8));
-                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
-                } else if (k1 % 8 == 0) {  // (uniform)
-                    w[i] = load_any(src + (at < k1 ? at : k1 - 8));
-                    if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
-                } else {
-                    w[i] = load_some(src + at, k1 - at);
-                }
+                if constexpr (CLEAN) w[i] = *reinterpret_cast<const u32x4v*>(src + (at < k1 ? at : k1 - 8));
+                else if (whole && !odd) w[i] = load_any(src + (at < k1 ? at : k1 - 8));
+                else if (whole) w[i] = load_dwords(src + (at < k1 ? at : k1 - 8));
+                else w[i] = load_some(src + at, k1 - at);
+                if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
             }
         }
     }
