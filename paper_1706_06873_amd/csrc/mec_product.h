@@ -452,17 +452,19 @@ __device__ inline void mirror(const Product& p, const floatx16& acc, int32_t m0,
     const int32_t m = m0 + (lane & 31);
     if (m >= p.M) return;
     const bool part = p.splits > 1;
+    float r[16] = {};
+    if (p.R && !part)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {  // all in flight at once, before any store that might change them
+            const int64_t n = n0 + acc_row(v, lane);
+            r[v] = static_cast<const float*>(p.R)[bat * p.r_batch + (n < p.N ? n : p.N - 1) * p.ldr + m];
+        }
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         const int64_t n = n0 + acc_row(v, lane);
         if (n >= p.N) continue;
-        if (part) {
-            p.part[(((int64_t)split * p.batch + bat) * p.M + n) * p.N + m] = acc[v];
-        } else {
-            float x = acc[v] * p.alpha;
-            if (p.R) x += p.beta * static_cast<const float*>(p.R)[bat * p.r_batch + n * p.ldr + m];
-            static_cast<float*>(p.Y)[bat * p.y_batch + n * p.ldy + m] = x;
-        }
+        if (part) p.part[(((int64_t)split * p.batch + bat) * p.M + n) * p.N + m] = acc[v];
+        else static_cast<float*>(p.Y)[bat * p.y_batch + n * p.ldy + m] = acc[v] * p.alpha + p.beta * r[v];
     }
 }
 // Tile t of those of a symmetric Y on and below the diagonal, row by row
