@@ -12,17 +12,22 @@ namespace {
 
 constexpr int kKT = 32, kG = kKT / 8;  // chunk of the reduction, groups of 8 in it
 
+// KW groups of WM x WN waves share the reduction of a tile, each with stages of its own: what
+// several tiles on a compute unit do for one another where there are that many (1024 x 1024 x
+// 4096, a tile per compute unit, 88 us, so 69; two groups likewise, but for short reductions).
 // TAIL: an operand stored along the reduction ends inside a group of 8.
-template <int BM, int BN, int WM, int WN, Layout L, bool TAIL>
+template <int BM, int BN, int WM, int WN, int KW, Layout L, bool TAIL>
 struct Cfg {
-    static constexpr int kBM = BM, kBN = BN, kWM = WM, kWN = WN;
+    static constexpr int kBM = BM, kBN = BN, kWM = WM, kWN = WN, kKW = KW;
     static constexpr bool kAT = L == Layout::kXtK, kBT = L != Layout::kXKt;  // stored across the reduction
     static constexpr bool kTail = TAIL;
-    static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;  // of a group
     static constexpr int APL = TM * kKT * 2, BPL = TN * kKT * 2, STAGE = 3 * (APL + BPL);  // bytes (of a plane)
     static constexpr int EPI = WAVES * 32 * (32 * BN + 4) * 4;
-    static constexpr int LDS = 2 * STAGE > EPI ? 2 * STAGE : EPI;
-    static constexpr int kPerSimd = WAVES == 8 ? 2 : (LDS <= 53 * 1024 ? 3 : LDS <= 80 * 1024 ? 2 : 1);
+    static constexpr int JOIN = (KW - 1) * WAVES * 4096;  // sums of a group's waves
+    static_assert(KW == 1 || (BM * BN == 1 && EPI + JOIN <= 2 * KW * STAGE), "groups");
+    static constexpr int LDS = 2 * KW * STAGE > EPI ? 2 * KW * STAGE : EPI;
+    static constexpr int kPerSimd = WAVES * KW >= 8 ? WAVES * KW / 4 : (LDS <= 53 * 1024 ? 3 : LDS <= 80 * 1024 ? 2 : 1);
     static_assert(TM * kG % THREADS == 0 && TN * kG % THREADS == 0 && THREADS % TM == 0 && THREADS % TN == 0 && LDS <= 158 * 1024, "tile");
 };
 
@@ -117,13 +122,15 @@ __device__ __attribute__((noinline)) floatx16 plain_block(const float* a, int64_
 }
 
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Product p) {
+__global__ __launch_bounds__(C::THREADS * C::kKW, C::kPerSimd) void product_f32_kernel(Product p) {
     constexpr int BM = C::kBM, BN = C::kBN;
     using OpA = Operand<C::TM, C::THREADS, C::kAT, C::kTail>;
     using OpB = Operand<C::TN, C::THREADS, C::kBT, C::kTail>;
-    __shared__ __align__(16) char lds[C::LDS];
+    __shared__ __align__(16) char all[C::LDS];
     __shared__ uint32_t lost_s;  // some thread's split left bits out
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = C::kKW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / C::THREADS) : 0;
+    const int tid = (int)threadIdx.x - group * C::THREADS, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char* const lds = all + group * 2 * C::STAGE;
     const int wm = wave % C::kWM, wn = wave / C::kWM;
     constexpr bool SQUARE = C::TM == C::TN && BM * BN == 1;  // holds symmetric products
     const bool symmetric = SQUARE && p.symmetric;
@@ -135,13 +142,15 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
     if (symmetric) tile_of_half(b - share * tiles, mt, nt);
     else tile_of(b - share * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
     const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
-    const int64_t k0 = (int64_t)split * p.chunks * kKT;
-    const int64_t k1 = k0 + (int64_t)p.chunks * kKT < p.K ? k0 + (int64_t)p.chunks * kKT : p.K;
-    const int chunks = (int)((k1 - k0 + kKT - 1) / kKT);
+    const int64_t s0 = (int64_t)split * p.chunks * kKT;  // the share, and this group's run of it (or none)
+    const int64_t s1 = s0 + (int64_t)p.chunks * kKT < p.K ? s0 + (int64_t)p.chunks * kKT : p.K;
+    const int chunks = (int)((s1 - s0 + C::kKW * kKT - 1) / (C::kKW * kKT));
+    const int64_t k0 = s0 + (int64_t)group * chunks * kKT < s1 ? s0 + (int64_t)group * chunks * kKT : s1;
+    const int64_t k1 = k0 + (int64_t)chunks * kKT < s1 ? k0 + (int64_t)chunks * kKT : s1;
     const float* const A = a_of<float>(p, bat);
     const float* const B = b_of<float>(p, bat);
 
-    if (tid == 0) lost_s = 0;  // (ordered by the first barriers)
+    if (threadIdx.x == 0) lost_s = 0;  // (ordered by the first barriers)
     OpA oa;
     OpB ob;
     oa.init(A, p.lda, m0, p.M, k0, k1, tid);
@@ -206,8 +215,9 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
         products(f);
         __syncthreads();
     };
-    for (int c = 0; c < chunks; c += 2) {  // (chunks past the last are zeros)
+    for (int c = 0; c < chunks; c += 2) {  // (chunks past the last are zeros, or another group's)
         step(lds, lds + C::STAGE);
+        if (C::kKW > 1 && c + 1 == chunks) break;
         step(lds + C::STAGE, lds);
     }
 
@@ -227,7 +237,7 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
             }
     if (lost & 0xffffu) lost_s = 1;
     __syncthreads();
-    float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * (32 * BN + 4);
+    float* const mine = reinterpret_cast<float*>(all) + wave * 32 * (32 * BN + 4);
     const int32_t mw = m0 + wm * BM * 32, nw = n0 + wn * BN * 32;
     if (lost_s || __any(most >= 0x7f800000u)) {
         const int64_t ars = C::kAT ? 1 : p.lda, aks = C::kAT ? p.lda : 1;
@@ -242,15 +252,34 @@ __global__ __launch_bounds__(C::THREADS, C::kPerSimd) void product_f32_kernel(Pr
                 acc[i][j] = plain_block(A + m * ars + k0 * aks, aks, B + n * brs + k0 * bks, bks, (int32_t)(k1 - k0), lane);
             }
     }
+    if constexpr (C::kKW > 1) {  // the groups' sums, joined in their order by the first
+        float* const sums = reinterpret_cast<float*>(all + C::EPI) + wave * 1024 + lane * 4;
+        if (group) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4v*>(sums + (group - 1) * C::WAVES * 1024 + q * 256) =
+                    f32x4v{acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < C::kKW; ++g)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4v s = *reinterpret_cast<const f32x4v*>(sums + (g - 1) * C::WAVES * 1024 + q * 256);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][4 * q + e] += s[e];
+            }
+    }
     if constexpr (SQUARE) {
         if (symmetric && mt != nt) mirror(p, acc[0][0], mw, nw, bat, split, lane);
     }
     epilogue<float, BM, BN>(p, acc, mine, mw, nw, bat, split, lane);
 }
 
-template <int BM, int BN, int WM, int WN, Layout L>
+template <int BM, int BN, int WM, int WN, int KW, Layout L>
 hipError_t run(Product p, hipStream_t stream) {
-    using C = Cfg<BM, BN, WM, WN, L, false>;
+    using C = Cfg<BM, BN, WM, WN, KW, L, false>;
     p.m_tiles = (p.M + C::TM - 1) / C::TM;
     p.n_tiles = (p.N + C::TN - 1) / C::TN;
     // shares are whole multiples of 64 elements, as plan_product counts them
@@ -261,21 +290,22 @@ hipError_t run(Product p, hipStream_t stream) {
     if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
     if constexpr (L != Layout::kXtK) {
         if (p.K % 8) {
-            using G = Cfg<BM, BN, WM, WN, L, true>;
-            hipLaunchKernelGGL(product_f32_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
+            using G = Cfg<BM, BN, WM, WN, KW, L, true>;
+            hipLaunchKernelGGL(product_f32_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS * KW), 0, stream, p);
             return hipGetLastError();
         }
     }
-    hipLaunchKernelGGL(product_f32_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
+    hipLaunchKernelGGL(product_f32_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS * KW), 0, stream, p);
     return hipGetLastError();
 }
 
 template <Layout L>
 hipError_t pick(const Product& p, int tile, hipStream_t stream) {
     switch (tile) {
-        case 1: return run<1, 2, 4, 1, L>(p, stream);
-        case 2: return run<2, 2, 4, 2, L>(p, stream);
-        case 3: return run<1, 1, 2, 2, L>(p, stream);
+        case 1: return run<1, 2, 4, 1, 1, L>(p, stream);
+        case 2: return run<2, 2, 4, 2, 1, L>(p, stream);
+        case 3: return run<1, 1, 2, 2, 1, L>(p, stream);
+        case 4: return run<1, 1, 2, 2, 3, L>(p, stream);
         default: return hipErrorNotSupported;
     }
 }

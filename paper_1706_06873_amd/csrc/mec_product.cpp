@@ -6,7 +6,8 @@
 // reductions over few and many tiles (M x N x K, us): bf16 16384 x 4096 x 4096 256x256 471,
 // 128x128 526, 64x128 619, 64x64 746; 1024 x 1024 x 1024 34, 16.0, 11.5, 8.5 and small 19;
 // 512 x 512 x 64 small 4.0, 128x128 7.4. fp32 16384 x 4096 x 1024 256x128 694, 128x64 862,
-// 64x64 928; 1024 x 1024 x 1024 69, 37, 26 and small 36; 512 x 512 x 512 small 6.7.
+// 64x64 928; 1024 x 1024 x 1024 69, 37, 25 (in three groups 22) and small 36; 512 x 512 x 512
+// small 6.7.
 #include "mec_product.h"
 
 namespace mec {
@@ -22,7 +23,8 @@ constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
                               {64, 128, 3, {0.40, 0.70, 0.85}, 3.5},
                               {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4},
                               {64, 64, 2, {0.26, 0.38}, 3.8}};
-constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0}};
+constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0},
+                             {64, 64, 1, {0.48}, 7.0}};
 
 constexpr int kSymmetricF32 = 3;  // the fp32 kernel with square tiles
 
@@ -40,7 +42,7 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
                          bool symmetric) {
     const TileCost* const tiles = dtype ? kBf16 : kF32;
-    const int count = dtype ? 5 : 3;
+    const int count = dtype ? 5 : 4;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
     // A call of one product in shares takes its caller's thread a second launch and a workspace
     // (13 us, so 8; 1 x 2048 x 1000 in bf16 in one launch 7.5 us, in shares 14.0): below that
@@ -67,7 +69,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
-            if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((real + (alone ? 1 : 0)) * batch * M * N) / 8e5;  // the sum of the shares
+            if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((real + (alone ? 1 : 0)) * batch * M * N) / 1.2e6;  // the sum of the shares
             offer(i + 1, real, us);
         }
     }
