@@ -19,16 +19,19 @@ struct Slice {
     int32_t k0, k1;  // this wave's run of the reduction
 };
 
+// a wave's sums to LDS
+__device__ inline void put_sums(const floatx16& acc, float* sums, int wave, int lane) {
+    float* const mine = sums + wave * 32 * kPitch + (lane & 31) * kPitch + (lane >> 5) * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4v*>(mine + q * 8) = f32x4v{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+}
+
 // The sums of the waves, joined: thread t finishes output (t / 32, t % 32).
 template <class E>
 __device__ inline void join(const Product& p, const floatx16& acc, float* sums, int32_t m0, int32_t n0, int32_t bat, int waves,
                             int wave, int lane) {
-    if (wave < waves) {
-        float* const mine = sums + wave * 32 * kPitch + (lane & 31) * kPitch + (lane >> 5) * 4;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<f32x4v*>(mine + q * 8) = f32x4v{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
-    }
+    if (wave < waves) put_sums(acc, sums, wave, lane);
     __syncthreads();
     const int m = (int)threadIdx.x / 32, n = (int)threadIdx.x % 32;
     if (m0 + m >= p.M || n0 + n >= p.N) return;
@@ -83,10 +86,58 @@ __device__ inline void fetch(const float* base, int64_t ld, int32_t k, int32_t k
     }
 }
 
+// A wave's 32 x 32 sums over k0 <= k < k1 (a multiple of 16 from each other, or k1 the last):
+// fa and fb fetch this lane's 8 k from k on of its row and of its column. U: steps of 16 k in
+// flight.
+template <int U, class FA, class FB>
+__device__ inline floatx16 run_f32(int32_t k0, int32_t k1, int lane, FA fa, FB fb) {
+    const int32_t half = 8 * (lane >> 5);
+    floatx16 acc = {}, low = {};
+    uint32_t lost = 0;
+    for (int32_t k = k0; k < k1; k += 16 * U) {
+        float x[U][8], y[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            fa(k + 16 * u + half, x[u]);
+            fb(k + 16 * u + half, y[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            u32x4 xs[3], ys[3];
+            split8(x[u], xs[0], xs[1], xs[2], lost);
+            split8(y[u], ys[0], ys[1], ys[2], lost);
+            auto mm = [&](int i, int j, floatx16& to) {
+                to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ys[j]), __builtin_bit_cast(bf16x8, xs[i]),
+                                                             to, 0, 0, 0);
+            };
+            mm(0, 0, acc);
+            mm(1, 0, low);
+            mm(0, 1, low);
+            mm(1, 1, low);
+            mm(2, 0, low);
+            mm(0, 2, low);
+        }
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        acc[v] += low[v];
+        const float x = acc[v];
+        const uint32_t bits = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+        most = bits > most ? bits : most;
+    }
+    if (__any((lost & 0xffffu) != 0) || __any(most >= 0x7f800000u)) {  // values the split does not hold
+        floatx16 sum = {};
+        plain_products(
+            sum, (uint32_t)(k1 - k0 + 15) / 16u, [&](uint32_t s, float* x) { fb(k0 + (int32_t)s * 16 + half, x); },
+            [&](uint32_t s, float* x) { fa(k0 + (int32_t)s * 16 + half, x); });
+        acc = sum;
+    }
+    return acc;
+}
 template <Layout L>
 __device__ inline void small_f32(const Product& p, uint32_t b0, float* sums) {
     constexpr bool AT = L == Layout::kXtK, BT = L != Layout::kXKt;
-    constexpr int U = 2;  // steps of 16 k in flight
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place t = place(p, b0, wave);
     floatx16 acc = {};
@@ -96,50 +147,92 @@ __device__ inline void small_f32(const Product& p, uint32_t b0, float* sums) {
         const int32_t n = t.n0 + (lane & 31) < p.N ? t.n0 + (lane & 31) : p.N - 1;
         const float* const a = a_of<float>(p, t.bat) + (AT ? (int64_t)m : m * p.lda);
         const float* const b = b_of<float>(p, t.bat) + (BT ? (int64_t)n : n * p.ldb);
-        floatx16 low = {};
-        uint32_t lost = 0;
-        for (int32_t k = t.k.k0; k < t.k.k1; k += 16 * U) {
-            float x[U][8], y[U][8];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                fetch<AT>(a, p.lda, k + 16 * u + 8 * (lane >> 5), t.k.k1, x[u]);
-                fetch<BT>(b, p.ldb, k + 16 * u + 8 * (lane >> 5), t.k.k1, y[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                u32x4 xs[3], ys[3];
-                split8(x[u], xs[0], xs[1], xs[2], lost);
-                split8(y[u], ys[0], ys[1], ys[2], lost);
-                auto mm = [&](int i, int j, floatx16& to) {
-                    to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ys[j]), __builtin_bit_cast(bf16x8, xs[i]),
-                                                                 to, 0, 0, 0);
-                };
-                mm(0, 0, acc);
-                mm(1, 0, low);
-                mm(0, 1, low);
-                mm(1, 1, low);
-                mm(2, 0, low);
-                mm(0, 2, low);
-            }
-        }
-        uint32_t most = 0;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            acc[v] += low[v];
-            const float x = acc[v];
-            const uint32_t bits = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
-            most = bits > most ? bits : most;
-        }
-        if (__any((lost & 0xffffu) != 0) || __any(most >= 0x7f800000u)) {  // values the split does not hold
-            floatx16 sum = {};
-            plain_products(
-                sum, (uint32_t)(t.k.k1 - t.k.k0 + 15) / 16u,
-                [&](uint32_t s, float* x) { fetch<BT>(b, p.ldb, t.k.k0 + (int32_t)s * 16 + 8 * (lane >> 5), t.k.k1, x); },
-                [&](uint32_t s, float* x) { fetch<AT>(a, p.lda, t.k.k0 + (int32_t)s * 16 + 8 * (lane >> 5), t.k.k1, x); });
-            acc = sum;
-        }
+        acc = run_f32<2>(
+            t.k.k0, t.k.k1, lane, [&](int32_t k, float* x) { fetch<AT>(a, p.lda, k, t.k.k1, x); },
+            [&](int32_t k, float* x) { fetch<BT>(b, p.ldb, k, t.k.k1, x); });
     }
     join<float>(p, acc, sums, t.m0, t.n0, t.bat, t.waves, wave, lane);
+}
+
+// A step of the orthogonalisation from A, X' = a X + P X (WIDE; else X P), P = b A + c A A, for m
+// up to 128: each workgroup makes the 32 rows of P that its 32 x 32 outputs need (16 waves: up
+// to 4 blocks of columns, the reduction in 4 runs) and keeps them in LDS for the product with
+// X. More arithmetic than P in a launch of its own, but a launch less to wait for (363 x 96: 6.9
+// us, P and X one after the other 11).
+template <bool WIDE>
+__global__ __launch_bounds__(64 * kWaves) void orth_step_kernel(OrthStep p) {
+    constexpr int kRow = kOrthStepMax + 4;
+    __shared__ __align__(16) float sums[kWaves * 32 * kPitch];
+    __shared__ __align__(16) float P[32 * kRow];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31;
+    const int tr = (int)threadIdx.x / 32, tc = (int)threadIdx.x % 32;
+    const uint32_t n_tiles = (uint32_t)(p.cols + 31) / 32, tiles = (uint32_t)((p.rows + 31) / 32) * n_tiles;
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x), bat = b / tiles, mt = (b - bat * tiles) / n_tiles;
+    const int32_t r0 = (int32_t)mt * 32, c0 = (int32_t)(b - bat * tiles - mt * n_tiles) * 32, own = WIDE ? r0 : c0, m = p.m;
+    const float* const A = p.A + (int64_t)bat * m * m;
+    const int64_t x_at = (int64_t)bat * p.rows * p.cols;
+    const float* const X = p.X + x_at;
+    auto last = [](int32_t i, int32_t n) { return i < n ? i : n - 1; };
+
+    // the wave's part of X, and what this thread adds
+    float x[8] = {};
+    const int32_t k2 = 16 * wave;
+    if (k2 < m) {
+        if constexpr (WIDE) fetch<true>(X + last(c0 + l, p.cols), p.cols, k2 + 8 * (lane >> 5), m, x);
+        else fetch<false>(X + (int64_t)last(r0 + l, p.rows) * p.cols, 0, k2 + 8 * (lane >> 5), m, x);
+    }
+    const bool stored = r0 + tr < p.rows && c0 + tc < p.cols;
+    const int64_t at = (int64_t)(r0 + tr) * p.cols + c0 + tc;
+    const float own_x = stored ? X[at] : 0.0f;
+
+    // P's rows
+    const int t = wave & 3, run = ((m + 15) / 16 + 3) / 4 * 16;  // column block, k of a run
+    const int32_t k0 = (wave >> 2) * run, k1 = k0 + run < m ? k0 + run : m;
+    float own_a[kOrthStepMax / 32];
+#pragma unroll
+    for (int i = 0; i < kOrthStepMax / 32; ++i)
+        own_a[i] = own + tr < m && i * 32 + tc < m ? A[(own + tr) * m + i * 32 + tc] : 0.0f;
+    if (t * 32 < m && k0 < k1) {
+        const float* const ra = A + last(own + l, m) * m;
+        const float* const rb = A + last(t * 32 + l, m) * m;  // (A is symmetric)
+        put_sums(run_f32<2>(
+                     k0, k1, lane, [&](int32_t k, float* v) { fetch<false>(ra, 0, k, k1, v); },
+                     [&](int32_t k, float* v) { fetch<false>(rb, 0, k, k1, v); }),
+                 sums, wave, lane);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOrthStepMax / 32; ++i) {
+        if (i * 32 >= m) break;
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float s = sums[(i + 4 * q) * 32 * kPitch + tr * kPitch + tc];
+            v += q * run < m ? s : 0.0f;
+        }
+        P[tr * kRow + i * 32 + tc] = own + tr < m && i * 32 + tc < m ? p.b * own_a[i] + p.c * v : 0.0f;
+    }
+    __syncthreads();
+
+    if (k2 < m) {
+        auto ours = [&](int32_t k, float* v) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = P[l * kRow + k + e];
+        };
+        auto theirs = [&](int32_t, float* v) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[e];
+        };
+        const floatx16 acc = WIDE ? run_f32<1>(k2, k2 + 16, lane, ours, theirs) : run_f32<1>(k2, k2 + 16, lane, theirs, ours);
+        put_sums(acc, sums, wave, lane);
+    }
+    __syncthreads();
+    if (!stored) return;
+    float v = 0.0f;
+    for (int w = 0; w * 16 < m; ++w) v += sums[w * 32 * kPitch + tr * kPitch + tc];
+    v += p.a * own_x;
+    if (p.bf16) static_cast<uint16_t*>(p.Y)[x_at + at] = from_float<uint16_t>(v);
+    else static_cast<float*>(p.Y)[x_at + at] = v;
 }
 
 // ---------------------------------------------------------------- bf16
@@ -320,6 +413,15 @@ uint32_t prepare(Product& p, Layout layout, int dtype) {
 }
 
 }  // namespace
+
+hipError_t launch_orth_step(const OrthStep& p, int32_t batch, hipStream_t stream) {
+    const int64_t blocks = (int64_t)((p.rows + 31) / 32) * ((p.cols + 31) / 32) * batch;
+    if (p.m > kOrthStepMax || p.m != (p.rows < p.cols ? p.rows : p.cols) || blocks > kMaxSmallBlocks) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)blocks), block(64 * kWaves);
+    if (p.rows <= p.cols) hipLaunchKernelGGL(orth_step_kernel<true>, grid, block, 0, stream, p);
+    else hipLaunchKernelGGL(orth_step_kernel<false>, grid, block, 0, stream, p);
+    return hipGetLastError();
+}
 
 hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream) {
     const uint32_t blocks = prepare(p, layout, dtype);

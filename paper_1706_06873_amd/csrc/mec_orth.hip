@@ -113,14 +113,26 @@ hipError_t normalise(const OrthParams& q, int32_t batch, hipStream_t stream) {
 
 int64_t round16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
-// m x m matrices for each of the stack: A, A after a step, P A (then P' P), P, P'; before the
-// first of them all but A hold the shares of its sum.
-constexpr int kSquares = 7;
+// m x m matrices for each of the stack: A, A after a step, P A (then P' P), P, P'; before those
+// all but A hold the shares of A's sum: 6, or up to 32 of small ones (32 MB).
+constexpr int kSquares = 5;
+int32_t gram_shares(int64_t m, int32_t batch) {
+    const int64_t fit = (int64_t(32) << 20) / (m * m * 4 * batch);
+    return (int32_t)(fit < 6 ? 6 : fit < 32 ? fit : 32);
+}
 
 // A pair of steps at once: the modelled times of the products that differ.
 bool pairs_preferred(int64_t m, int64_t n, int32_t batch) {
     auto us = [&](int64_t M, int64_t N, int64_t K) { return plan_product(Layout::kXKt, 0, M, N, K, batch, 1, M == N).us; };
     return us(m, m, n) + us(n, m, m) > 3 * us(m, m, m);
+}
+
+// The polynomial and the product with X in one launch: where the polynomial's rows, made again
+// for every 32 x 32 outputs, cost less than a launch: one round of workgroups (363 x 96 88 us
+// without, so 70; 8 of 64 x 1000, two rounds, 100 and 112), and pairs of steps do not save
+// more on A (5000 x 32 119 and 129).
+bool step_preferred(int64_t m, int64_t rows, int64_t cols, int32_t batch) {
+    return m <= kOrthStepMax && rows <= 2048 && cols <= 2048 && ((rows + 31) / 32) * ((cols + 31) / 32) * batch <= 256;
 }
 
 }  // namespace
@@ -129,7 +141,8 @@ bool pairs_preferred(int64_t m, int64_t n, int32_t batch) {
 // last use.
 int64_t orth_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int) {
     const int64_t m = rows < cols ? rows : cols;
-    return 16 + 2 * round16(batch * rows * cols * 4) + kSquares * round16(batch * m * m * 4) + (int64_t)batch * kShares * 8;
+    return 16 + 2 * round16(batch * rows * cols * 4) +
+           (1 + gram_shares(m, batch)) * round16(batch * m * m * 4) + (int64_t)batch * kShares * 8;
 }
 
 hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, int64_t rows, int64_t cols, int32_t steps,
@@ -144,7 +157,9 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
     };
     float* const X[2] = {take(batch * m * n * 4), take(batch * m * n * 4)};
     float* S[kSquares];
-    for (float*& s : S) s = take(batch * mm * 4);  // one after another: S[1] on holds kSquares - 1 of them
+    const int32_t shares = gram_shares(m, batch);
+    for (float*& s : S) s = take(batch * mm * 4);
+    take((1 + shares - kSquares) * round16(batch * mm * 4));  // S[1] on holds the shares
 
     OrthParams q{};
     q.U = U;
@@ -177,7 +192,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         e = launch_product(Layout::kXKt, p, 0, stream);
     };
     int copy = 0;
-    const bool pairs = pairs_preferred(m, n, batch);
+    const bool one = step_preferred(m, rows, cols, batch), pairs = !one && pairs_preferred(m, n, batch);
     for (int32_t left = steps; left > 0 && e == hipSuccess;) {
         const bool two = pairs && left >= 2 && (left == steps || left == 2);
         left -= two ? 2 : 1;
@@ -195,9 +210,16 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.symmetric = 1;
         p.part = S[1];  // the other squares are free now
         const Layout gram = wide ? Layout::kXKt : Layout::kXtK;
-        const ProductPlan plan = plan_product(gram, 0, m, m, n, batch, kSquares - 1, true);
+        const ProductPlan plan = plan_product(gram, 0, m, m, n, batch, shares, true);
         e = launch_product(plan, gram, p, 0, stream);
         if (e == hipSuccess && plan.splits > 1) e = launch_sum_parts(S[1], plan.splits, batch * mm, A, 0, stream);
+        copy ^= 1;
+        void* const to = left ? static_cast<void*>(X[copy]) : O;
+        if (one) {
+            if (e == hipSuccess)
+                e = launch_orth_step({A, from, to, (int32_t)m, (int32_t)rows, (int32_t)cols, !left && dtype, a, b, c}, batch, stream);
+            continue;
+        }
         square(A, A, P, c, A, b, two ? a : 0.0f);  // a single step adds a X itself
         if (two) {
             square(P, A, T, 1.0f, nullptr, 0.0f, 0.0f);
@@ -212,7 +234,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
             p.R = from;
             p.beta = a;
         }
-        p.Y = left ? static_cast<void*>(X[copy ^ 1]) : O;
+        p.Y = to;
         p.y_bf16 = !left && dtype;
         p.M = (int32_t)rows;
         p.N = (int32_t)cols;
@@ -226,7 +248,6 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.ldb = wide ? cols : m;
         p.b_batch = wide ? m * n : mm;
         e = launch_product(wide ? Layout::kXK : Layout::kXKt, p, 0, stream);
-        copy ^= 1;
     }
     return e;
 }

@@ -60,6 +60,16 @@ hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t s
 hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream);   // mec_linear_f32.hip
 constexpr int64_t kMaxSmallBlocks = 0x1fffff;  // of 1024 threads, in a launch
 hipError_t launch_product_small(Layout layout, Product p, int dtype, hipStream_t stream);  // mec_linear_small.hip
+// A step of the orthogonalisation from A = X X^T or X^T X (m x m) in one launch.
+constexpr int kOrthStepMax = 128;  // m
+struct OrthStep {
+    const float* A;
+    const float* X;
+    void* Y;  // not X; bf16 where bf16
+    int32_t m, rows, cols, bf16;
+    float a, b, c;
+};
+hipError_t launch_orth_step(const OrthStep& p, int32_t batch, hipStream_t stream);
 // two small products, x of layout kXKt and k of kXtK, in one launch
 hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream);
 // by the plan, in one share
