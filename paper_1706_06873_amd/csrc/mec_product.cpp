@@ -26,7 +26,7 @@ constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
 constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0},
                              {64, 64, 1, {0.48}, 7.0}};
 
-constexpr int kSymmetricF32 = 3;  // the fp32 kernel with square tiles
+constexpr int kSymmetricF32 = 3;  // the fp32 kernels from this one on have square tiles
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -62,14 +62,16 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K));
     for (int i = 0; i < count; ++i) {
         int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn);
-        if (symmetric && !dtype && i + 1 == kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
+        if (symmetric && !dtype && i + 1 >= kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
         n *= batch;
         for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
             // shares of at least 4 chunks of 64, none empty, and partial sums of at most 256 MB
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
-            if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((real + (alone ? 1 : 0)) * batch * M * N) / 1.2e6;  // the sum of the shares
+            // the sum of the shares: a launch, its reads, and what else moves (the epilogue's
+            // output; a mirror image's 4-byte stores)
+            if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((alone ? real + 1 : symmetric ? 2 * real : real) * batch * M * N) / 1.2e6;
             offer(i + 1, real, us);
         }
     }
@@ -78,7 +80,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
 
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {
     p.splits = plan.splits;
-    p.symmetric = p.symmetric && !dtype && plan.kernel == kSymmetricF32;
+    p.symmetric = p.symmetric && !dtype && plan.kernel >= kSymmetricF32;
     if (plan.kernel == 0) return p.splits > 1 ? hipErrorNotSupported : launch_product_small(layout, p, dtype, stream);
     return dtype ? launch_product_bf16(layout, p, plan.kernel, stream) : launch_product_f32(layout, p, plan.kernel, stream);
 }
