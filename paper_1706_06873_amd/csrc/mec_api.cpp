@@ -357,6 +357,10 @@ constexpr int32_t kMaxShares = 64;  // of a product's reduction
 // the sums of a product's shares
 int64_t parts_bytes(const mec::ProductPlan& plan, int64_t M, int64_t N) { return plan.splits > 1 ? plan.splits * M * N * 4 : 0; }
 
+int64_t linear_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
+    return parts_bytes(mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares), rows, k_c);
+}
+
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
     const int64_t dx = parts_bytes(mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares), rows, i_c);
     const int64_t dk = parts_bytes(mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares), i_c, k_c);
@@ -377,10 +381,8 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     const int64_t es = elem_bytes(dtype);
     if (!aligned(X, es) || !aligned(K, es) || !aligned(bias, 4) || !aligned(R, es) || !aligned(Y, es) || !aligned(Z, es))
         return MEC_ERR_ALIGNMENT;
-    const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares);
-    if (plan.splits > 1 &&
-        (!workspace || (uint64_t)workspace_bytes < (uint64_t)parts_bytes(plan, rows, k_c)))
-        return MEC_ERR_WORKSPACE;
+    const int64_t need = linear_bytes(rows, i_c, k_c, dtype);
+    if (need && (!workspace || (uint64_t)workspace_bytes < (uint64_t)need)) return MEC_ERR_WORKSPACE;
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     mec::Product p{};
     p.A = X;
@@ -402,6 +404,7 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     p.batch = 1;
     p.part = static_cast<float*>(workspace);
     clear_stale_error();
+    const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXK, dtype, p, kMaxShares);
     return hip_status(launch_shared(plan, mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
 }
 
@@ -409,7 +412,7 @@ int64_t mec_linear_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
     const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
     if (rc != MEC_OK) return rc;
     if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
-    return parts_bytes(mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares), rows, k_c);
+    return linear_bytes(rows, i_c, k_c, dtype);
 }
 
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
@@ -468,8 +471,8 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     k.K = (int32_t)rows;
     k.part = part;
     x.part = part;
-    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x.M, x.N, x.K, 1, kMaxShares);
-    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k.M, k.N, k.K, 1, kMaxShares);
+    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x, kMaxShares);
+    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k, kMaxShares);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
     if (dX) {

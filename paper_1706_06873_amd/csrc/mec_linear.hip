@@ -353,10 +353,7 @@ hipError_t pick(const Product& p, int tile, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream) {
-    auto rows16 = [](const void* base, int64_t ld) { return !base || (((uintptr_t)base & 15u) == 0 && ld % 8 == 0); };
-    // the dimension that each operand's rows run along has to be whole granules
-    const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
-    p.clean = rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;
+    p.clean = clean_rows(layout, p);
     switch (layout) {
         case Layout::kXK: return pick<Layout::kXK>(p, tile, stream);
         case Layout::kXKt: return pick<Layout::kXKt>(p, tile, stream);

@@ -404,11 +404,7 @@ uint32_t prepare(Product& p, Layout layout, int dtype) {
     // a wave's run: whole steps of 16 k
     const int64_t steps = ((int64_t)p.K + 15) / 16;
     p.chunks = (int32_t)((steps + kWaves - 1) / kWaves);
-    if (dtype) {
-        const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
-        p.clean = !(((uintptr_t)p.A | (uintptr_t)p.B) & 15u) && p.lda % 8 == 0 && p.ldb % 8 == 0 && a_run % 8 == 0 &&
-                  b_run % 8 == 0 && p.a_batch % 8 == 0 && p.b_batch % 8 == 0;
-    }
+    if (dtype) p.clean = clean_rows(layout, p) && p.a_batch % 8 == 0 && p.b_batch % 8 == 0;
     return blocks > kMaxSmallBlocks || p.splits > 1 ? 0 : (uint32_t)blocks;
 }
 

@@ -19,10 +19,16 @@ struct TileCost {
 };
 // by the kernels' numbers, from 1
 constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
-                              {256, 256, 1, {1.45}, 8.5},
+                              {256, 256, 1, {1.45}, 11.0},
                               {64, 128, 3, {0.40, 0.70, 0.85}, 3.5},
                               {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4},
                               {64, 64, 2, {0.26, 0.38}, 3.8}};
+// the same by way of registers (rows that are no whole 16-byte granules): 1886 x 3185 -> 2368
+// 95, 157, 81, 110 where 3184 takes 50, 62, 50, 62; 11471 x 2505 -> 48 65, 124, 51, 43
+constexpr TileCost kBf16Any[] = {{128, 128, 2, {1.50, 1.80}, 4.2},
+                                 {256, 256, 1, {2.90}, 11.0},
+                                 {64, 128, 3, {1.19, 1.35, 1.55}, 3.5},
+                                 {64, 64, 5, {0.80, 1.10, 1.45, 1.80, 2.10}, 3.4}};
 constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0},
                              {64, 64, 1, {0.48}, 7.0}};
 
@@ -40,9 +46,9 @@ double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
 }  // namespace
 
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
-                         bool symmetric) {
-    const TileCost* const tiles = dtype ? kBf16 : kF32;
-    const int count = dtype ? 5 : 4;
+                         bool symmetric, bool clean) {
+    const TileCost* const tiles = !dtype ? kF32 : clean ? kBf16 : kBf16Any;
+    const int count = dtype && clean ? 5 : 4;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
     // A call of one product in shares takes its caller's thread a second launch and a workspace
     // (13 us, so 8; 1 x 2048 x 1000 in bf16 in one launch 7.5 us, in shares 14.0): below that
@@ -58,8 +64,9 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
             best = {kernel, (int32_t)splits, us};
         }
     };
+    const double per_k = !dtype ? 0.0066 : clean ? 0.0027 : layout == Layout::kXKt ? 0.0075 : 0.0040;
     const int64_t small = ceil_div(M, 32) * ceil_div(N, 32) * batch;
-    if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + (dtype ? 0.0027 : 0.0066) * (double)K));
+    if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + per_k * (double)K));
     for (int i = 0; i < count; ++i) {
         int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn);
         if (symmetric && !dtype && i + 1 >= kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
@@ -76,6 +83,18 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
         }
     }
     return best;
+}
+
+bool clean_rows(Layout layout, const Product& p) {
+    auto rows16 = [](const void* base, int64_t ld) { return ((uintptr_t)base & 15u) == 0 && ld % 8 == 0; };
+    // the dimension that each operand's rows run along has to be whole granules
+    const int64_t a_run = layout == Layout::kXtK ? p.M : p.K, b_run = layout == Layout::kXKt ? p.K : p.N;
+    return rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;
+}
+
+ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits) {
+    const ProductPlan plan = plan_product(layout, dtype, p.M, p.N, p.K, 1, max_splits);
+    return !dtype || clean_rows(layout, p) ? plan : plan_product(layout, dtype, p.M, p.N, p.K, 1, plan.splits, false, false);
 }
 
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {

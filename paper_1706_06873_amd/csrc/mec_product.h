@@ -49,9 +49,14 @@ struct ProductPlan {
     int32_t splits;
     double us;   // by the model
 };
-// max_splits: as many shares as the caller has room for partial sums (batch x M x N each)
+// max_splits: as many shares as the caller has room for partial sums (batch x M x N each);
+// clean: 16-byte rows
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
-                         bool symmetric = false);
+                         bool symmetric = false, bool clean = true);
+// one product on its operands as they lie, in no more shares than the first takes by the sizes alone
+ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits);
+// A's and B's rows are whole 16-byte granules (bf16)
+bool clean_rows(Layout layout, const Product& p);
 
 // Enqueue the product (dtype of A, B, Z, R, Y), with p.splits shares that leave their partial
 // sums where it is above 1. hipErrorNotSupported where there is no such kernel.
