@@ -224,7 +224,8 @@ def _time_block(layer, dtype, reps, warmup):
     dK = 1e-3 * randn(k_h, k_w, i_c, c)
     stream = torch.cuda.Stream(device=dev)
     code = mec.BF16 if dtype == "bf16" else mec.F32
-    ws = torch.empty(max(mec.linear_grad_workspace_bytes(rows, c, wide, code),
+    ws = torch.empty(max(mec.linear_workspace_bytes(rows, c, wide, code), mec.linear_workspace_bytes(rows, wide, c, code),
+                         mec.linear_grad_workspace_bytes(rows, c, wide, code),
                          mec.linear_grad_workspace_bytes(rows, wide, c, code),
                          mec.layer_norm_grad_workspace_bytes(rows, c, code),
                          mec.orthogonalize_workspace_bytes(1, k_h * k_w * i_c, c)), dtype=torch.uint8, device=dev)
@@ -239,8 +240,8 @@ def _time_block(layer, dtype, reps, warmup):
         dg, db, db1, db2 = (torch.empty_like(t) for t in (gamma, beta, b1, b2))
     steps = {
         "norm": lambda: mec.layer_norm(X, gamma, beta, Y=N, mean=mean, rstd=rstd),
-        "widen": lambda: mec.linear(N, K1, b1, act="gelu", Y=H, Z=Z),
-        "narrow": lambda: mec.linear(H, K2, b2, residual=X, Y=Y),
+        "widen": lambda: mec.linear(N, K1, b1, act="gelu", Y=H, Z=Z, workspace=ws),
+        "narrow": lambda: mec.linear(H, K2, b2, residual=X, Y=Y, workspace=ws),
         "narrow_grad": lambda: mec.linear_grad(G, H, K2, dX=dH, dK=dK2, dbias=db2, workspace=ws),
         "widen_grad": lambda: mec.linear_grad(dH, N, K1, Z, "gelu", dZ=dZ, dX=dX, dK=dK1, dbias=db1, workspace=ws),
         "norm_grad": lambda: mec.layer_norm_grad(G, X, mean, rstd, gamma, dX=dX, dgamma=dg, dbeta=db, workspace=ws),
