@@ -15,38 +15,44 @@ namespace {
 
 struct TileCost {
     int tm, tn, fit;
-    double chunk[5], ends;
+    double chunk[5], ends, residual, saved;  // residual, saved: what R and Z add to the ends
 };
-// by the kernels' numbers, from 1
-constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2},
-                              {256, 256, 1, {1.45}, 11.0},
-                              {64, 128, 3, {0.40, 0.70, 0.85}, 3.5},
-                              {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4},
-                              {64, 64, 2, {0.26, 0.38}, 3.8}};
+// by the kernels' numbers, from 1. Large tiles wait longer for a residual than small ones, of
+// which others run meanwhile: 1577088 x 64 -> 256 in bf16 281, 239, 297, 367 us, with Z 440, 409,
+// 458, 555, with R 415, 367, 329, 365, with both 531, 496, 455, 499; in fp32 744, 661, 804, with Z
+// 1128, 1000, 1219, with R 833, 819, 970, with both 1031, 1087, 1178.
+constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2, 2.5, 3.6},
+                              {256, 256, 1, {1.45}, 8.5, 5.3, 6.8},
+                              {64, 128, 3, {0.40, 0.70, 0.85}, 3.5, 0.4, 2.2},
+                              {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4, 0.0, 2.2},
+                              {64, 64, 2, {0.26, 0.38}, 3.8, 0.4, 1.0}};
 // the same by way of registers (rows that are no whole 16-byte granules): 1886 x 3185 -> 2368
 // 95, 157, 81, 110 where 3184 takes 50, 62, 50, 62; 11471 x 2505 -> 48 65, 124, 51, 43
-constexpr TileCost kBf16Any[] = {{128, 128, 2, {1.50, 1.80}, 4.2},
-                                 {256, 256, 1, {2.90}, 11.0},
-                                 {64, 128, 3, {1.19, 1.35, 1.55}, 3.5},
-                                 {64, 64, 5, {0.80, 1.10, 1.45, 1.80, 2.10}, 3.4}};
-constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 5.0}, {256, 128, 1, {2.3}, 12.0}, {64, 64, 3, {0.64, 0.95, 1.15}, 5.0},
-                             {64, 64, 1, {0.48}, 7.0}};
+constexpr TileCost kBf16Any[] = {{128, 128, 2, {1.50, 1.80}, 4.2, 2.5, 3.6},
+                                 {256, 256, 1, {2.90}, 8.5, 5.3, 6.8},
+                                 {64, 128, 3, {1.19, 1.35, 1.55}, 3.5, 0.4, 2.2},
+                                 {64, 64, 5, {0.80, 1.10, 1.45, 1.80, 2.10}, 3.4, 0.0, 2.2}};
+constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 4.8, 0.9, 3.2},
+                             {256, 128, 1, {2.3}, 10.0, 3.3, 6.5},
+                             {64, 64, 3, {0.64, 0.95, 1.15}, 5.0, 1.0, 2.5},
+                             {64, 64, 1, {0.48}, 7.0, 1.0, 2.5}};
 
 constexpr int kSymmetricF32 = 3;  // the fp32 kernels from this one on have square tiles
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-double tile_time(const TileCost& t, int64_t tiles, int64_t chunks) {
+double tile_time(const TileCost& t, int64_t tiles, int64_t chunks, double ends) {
     const int64_t busiest = ceil_div(tiles, 256), rounds = busiest / t.fit, rest = busiest % t.fit;
-    double us = (double)rounds * ((double)chunks * t.chunk[t.fit - 1] + t.ends);
-    if (rest) us += (double)chunks * t.chunk[rest - 1] + t.ends;
+    double us = (double)rounds * ((double)chunks * t.chunk[t.fit - 1] + ends);
+    if (rest) us += (double)chunks * t.chunk[rest - 1] + ends;
     return us;
 }
 
 }  // namespace
 
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
-                         bool symmetric, bool clean) {
+                         bool symmetric, const Operands& with) {
+    const bool clean = with.clean;
     const TileCost* const tiles = !dtype ? kF32 : clean ? kBf16 : kBf16Any;
     const int count = dtype && clean ? 5 : 4;
     const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
@@ -75,7 +81,8 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
             // shares of at least 4 chunks of 64, none empty, and partial sums of at most 256 MB
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
-            double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks);
+            const double ends = tiles[i].ends + (s > 1 ? 0.0 : (with.R ? tiles[i].residual : 0.0) + (with.Z ? tiles[i].saved : 0.0));
+            double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks, ends);
             // the sum of the shares: a launch, its reads, and what else moves (the epilogue's
             // output; a mirror image's 4-byte stores)
             if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((alone ? real + 1 : symmetric ? 2 * real : real) * batch * M * N) / 1.2e6;
@@ -94,7 +101,8 @@ bool clean_rows(Layout layout, const Product& p) {
 
 ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits) {
     const ProductPlan plan = plan_product(layout, dtype, p.M, p.N, p.K, 1, max_splits);
-    return !dtype || clean_rows(layout, p) ? plan : plan_product(layout, dtype, p.M, p.N, p.K, 1, plan.splits, false, false);
+    const Operands with{!dtype || clean_rows(layout, p), p.R != nullptr, p.Z != nullptr};
+    return with.clean && !with.R && !with.Z ? plan : plan_product(layout, dtype, p.M, p.N, p.K, 1, plan.splits, false, with);
 }
 
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {

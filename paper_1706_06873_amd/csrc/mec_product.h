@@ -49,10 +49,13 @@ struct ProductPlan {
     int32_t splits;
     double us;   // by the model
 };
-// max_splits: as many shares as the caller has room for partial sums (batch x M x N each);
-// clean: 16-byte rows
+// What the sizes do not say: 16-byte rows (clean), a residual, a saved argument of the activation.
+struct Operands {
+    bool clean = true, R = false, Z = false;
+};
+// max_splits: as many shares as the caller has room for partial sums (batch x M x N each)
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
-                         bool symmetric = false, bool clean = true);
+                         bool symmetric = false, const Operands& with = {});
 // one product on its operands as they lie, in no more shares than the first takes by the sizes alone
 ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits);
 // A's and B's rows are whole 16-byte granules (bf16)
