@@ -364,9 +364,10 @@ int64_t linear_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
 int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
     const int64_t dx = parts_bytes(mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares), rows, i_c);
     const int64_t dk = parts_bytes(mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares), i_c, k_c);
+    const int64_t pair = parts_bytes(mec::plan_pair(dtype, rows, i_c, k_c, kMaxShares), i_c, k_c);
     const int64_t shares = mec::act_grad_shares(rows, k_c);  // one share goes straight to dbias
     const int64_t db = shares > 1 ? shares * k_c * 4 : 0;
-    return std::max({dx, dk, db});
+    return std::max({dx, dk, pair, db});
 }
 
 }  // namespace
@@ -475,6 +476,16 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k, kMaxShares);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
+    if (dX && dK) {
+        const mec::ProductPlan pair = mec::plan_pair(dtype, rows, i_c, k_c, kMaxShares);
+        if (pair.kernel) {
+            k.splits = pair.splits;
+            rc = hip_status(mec::launch_product_f32_pair(x, k, st), "gradients of the input and the kernel");
+            if (rc == MEC_OK && k.splits > 1)
+                rc = hip_status(mec::launch_sum_parts(part, k.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
+            return rc;
+        }
+    }
     if (dX) {
         rc = hip_status(launch_shared(px, mec::Layout::kXKt, x, dtype, st), "gradient of the input");
         if (rc != MEC_OK) return rc;

@@ -121,13 +121,13 @@ __device__ __attribute__((noinline)) floatx16 plain_block(const float* a, int64_
     return sum;
 }
 
+// Workgroup b's tile. all: C::LDS bytes of LDS; lost_s, there too: some thread's split left
+// bits out.
 template <class C>
-__global__ __launch_bounds__(C::THREADS * C::kKW, C::kPerSimd) void product_f32_kernel(Product p) {
+__device__ inline void product_f32(const Product& p, uint32_t b, char* all, uint32_t& lost_s) {
     constexpr int BM = C::kBM, BN = C::kBN;
     using OpA = Operand<C::TM, C::THREADS, C::kAT, C::kTail>;
     using OpB = Operand<C::TN, C::THREADS, C::kBT, C::kTail>;
-    __shared__ __align__(16) char all[C::LDS];
-    __shared__ uint32_t lost_s;  // some thread's split left bits out
     const int group = C::kKW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / C::THREADS) : 0;
     const int tid = (int)threadIdx.x - group * C::THREADS, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char* const lds = all + group * 2 * C::STAGE;
@@ -135,7 +135,6 @@ __global__ __launch_bounds__(C::THREADS * C::kKW, C::kPerSimd) void product_f32_
     constexpr bool SQUARE = C::TM == C::TN && BM * BN == 1;  // holds symmetric products
     const bool symmetric = SQUARE && p.symmetric;
     const uint32_t tiles = symmetric ? (uint32_t)p.m_tiles * ((uint32_t)p.m_tiles + 1) / 2 : (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
-    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
     const uint32_t share = b / tiles;  // of the reduction, for each product of a batch
     const int32_t split = (int32_t)(share / (uint32_t)p.batch), bat = (int32_t)(share - (uint32_t)split * (uint32_t)p.batch);
     uint32_t mt, nt;
@@ -277,9 +276,27 @@ __global__ __launch_bounds__(C::THREADS * C::kKW, C::kPerSimd) void product_f32_
     epilogue<float, BM, BN>(p, acc, mine, mw, nw, bat, split, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int KW, Layout L>
-hipError_t run(Product p, hipStream_t stream) {
-    using C = Cfg<BM, BN, WM, WN, KW, L, false>;
+template <class C>
+__global__ __launch_bounds__(C::THREADS * C::kKW, C::kPerSimd) void product_f32_kernel(Product p) {
+    __shared__ __align__(16) char all[C::LDS];
+    __shared__ uint32_t lost_s;
+    product_f32<C>(p, xcd_remap(blockIdx.x, gridDim.x), all, lost_s);
+}
+
+// The two products of a backward pass, dX = dZ K^T and dK = X^T dZ, side by side in one launch: the
+// tiles of one fill the compute units that the other's last round leaves.
+template <class X, class K>
+__global__ __launch_bounds__(X::THREADS, X::kPerSimd) void product_f32_pair_kernel(Product x, Product k, uint32_t x_blocks) {
+    static_assert(X::LDS == K::LDS && X::kKW == 1 && K::kKW == 1, "one shape of tiles");
+    __shared__ __align__(16) char all[X::LDS];
+    __shared__ uint32_t lost_s;
+    if (blockIdx.x < x_blocks) product_f32<X>(x, xcd_remap(blockIdx.x, x_blocks), all, lost_s);
+    else product_f32<K>(k, xcd_remap(blockIdx.x - x_blocks, gridDim.x - x_blocks), all, lost_s);
+}
+
+// Fills what the kernels need; the workgroups, or 0 past the grid or for shares that leave some empty.
+template <class C>
+uint32_t prepare(Product& p) {
     p.m_tiles = (p.M + C::TM - 1) / C::TM;
     p.n_tiles = (p.N + C::TN - 1) / C::TN;
     // shares are whole multiples of 64 elements, as plan_product counts them
@@ -287,15 +304,22 @@ hipError_t run(Product p, hipStream_t stream) {
     p.chunks = 2 * (int32_t)((chunks / 2 + p.splits - 1) / p.splits);
     const int64_t tiles = p.symmetric ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles;
     const int64_t blocks = tiles * p.splits * p.batch;
-    if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
+    return blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
+}
+
+template <int BM, int BN, int WM, int WN, int KW, Layout L>
+hipError_t run(Product p, hipStream_t stream) {
+    using C = Cfg<BM, BN, WM, WN, KW, L, false>;
+    const uint32_t blocks = prepare<C>(p);
+    if (!blocks) return hipErrorInvalidValue;
     if constexpr (L != Layout::kXtK) {
         if (p.K % 8) {
             using G = Cfg<BM, BN, WM, WN, KW, L, true>;
-            hipLaunchKernelGGL(product_f32_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS * KW), 0, stream, p);
+            hipLaunchKernelGGL(product_f32_kernel<G>, dim3(blocks), dim3(G::THREADS * KW), 0, stream, p);
             return hipGetLastError();
         }
     }
-    hipLaunchKernelGGL(product_f32_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS * KW), 0, stream, p);
+    hipLaunchKernelGGL(product_f32_kernel<C>, dim3(blocks), dim3(C::THREADS * KW), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -311,6 +335,18 @@ hipError_t pick(const Product& p, int tile, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_product_f32_pair(Product x, Product k, hipStream_t stream) {
+    using X = Cfg<1, 1, 2, 2, 1, Layout::kXKt, false>;
+    using XTail = Cfg<1, 1, 2, 2, 1, Layout::kXKt, true>;
+    using K = Cfg<1, 1, 2, 2, 1, Layout::kXtK, false>;
+    const uint32_t bx = prepare<X>(x), bk = prepare<K>(k);
+    if (!bx || !bk || bx > 0x7fffffffu - bk) return hipErrorInvalidValue;
+    const dim3 grid(bx + bk), block(X::THREADS);
+    if (x.K % 8) hipLaunchKernelGGL((product_f32_pair_kernel<XTail, K>), grid, block, 0, stream, x, k, bx);
+    else hipLaunchKernelGGL((product_f32_pair_kernel<X, K>), grid, block, 0, stream, x, k, bx);
+    return hipGetLastError();
+}
 
 hipError_t launch_product_f32(Layout layout, Product p, int tile, hipStream_t stream) {
     switch (layout) {

@@ -92,6 +92,31 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     return best;
 }
 
+ProductPlan plan_pair(int dtype, int64_t rows, int64_t i_c, int64_t k_c, int32_t max_splits) {
+    ProductPlan best{0, 1, 0.0};
+    if (dtype) return best;
+    // what two launches take, by their models and a launch's own 3 us; the model of the pair is a
+    // little too high (1000 x 1000 x 1000 49 where it took 44, two launches 50; 4608 x 256 x 1024
+    // 57, 53 and 62; 20000 x 256 x 1024 166, 177 and 160; 11679 x 920 x 1619 508, 549 and 467)
+    best.us = 3.0 + 1.05 * (plan_product(Layout::kXKt, dtype, rows, i_c, k_c, 1, max_splits).us +
+                            plan_product(Layout::kXtK, dtype, i_c, k_c, rows, 1, max_splits).us);
+    const TileCost& t = kF32[kSymmetricF32 - 1];
+    const int64_t nx = ceil_div(rows, t.tm) * ceil_div(i_c, t.tn), nk = ceil_div(i_c, t.tm) * ceil_div(k_c, t.tn);
+    const int64_t shares = ceil_div(rows, 64);
+    auto tile = [&](int64_t chunks) { return (double)chunks * t.chunk[t.fit - 1] + t.ends; };
+    for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
+        if (s > 1 && (shares < 4 * s || s * i_c * k_c > (int64_t(1) << 26))) break;
+        const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
+        const double x = tile(ceil_div(k_c, 32)), k = tile(real > 1 ? 2 * per : ceil_div(rows, 32));
+        // the compute units are full but for the last tile's time
+        double us = ((double)nx * x + (double)(nk * real) * k) / (256.0 * t.fit);
+        us += 0.5 * (x > k ? x : k);
+        if (real > 1) us += 3.0 + (double)(real * i_c * k_c) / 1.2e6;
+        if (us < best.us) best = {kSymmetricF32, (int32_t)real, us};
+    }
+    return best;
+}
+
 bool clean_rows(Layout layout, const Product& p) {
     auto rows16 = [](const void* base, int64_t ld) { return ((uintptr_t)base & 15u) == 0 && ld % 8 == 0; };
     // the dimension that each operand's rows run along has to be whole granules

@@ -58,6 +58,9 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
                          bool symmetric = false, const Operands& with = {});
 // one product on its operands as they lie, in no more shares than the first takes by the sizes alone
 ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits);
+// dX (rows x i_c) and dK (i_c x k_c) of fp32 by tiles in one launch: kernel 3 and dK's shares, or
+// kernel 0 where two launches are as fast
+ProductPlan plan_pair(int dtype, int64_t rows, int64_t i_c, int64_t k_c, int32_t max_splits);
 // A's and B's rows are whole 16-byte granules (bf16)
 bool clean_rows(Layout layout, const Product& p);
 
@@ -78,7 +81,9 @@ struct OrthStep {
     float a, b, c;
 };
 hipError_t launch_orth_step(const OrthStep& p, int32_t batch, hipStream_t stream);
-// two small products, x of layout kXKt and k of kXtK, in one launch
+// the two products of a backward pass, x of layout kXKt (in one share) and k of kXtK, in one launch:
+// by 64 x 64 tiles, or both small
+hipError_t launch_product_f32_pair(Product x, Product k, hipStream_t stream);
 hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream);
 // by the plan, in one share
 hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream);

@@ -100,7 +100,8 @@ def test_linear(dtype, rows, i_c, k_c):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,i_c,k_c", SIZES + [(5000, 40, 24), (9001, 33, 130), (4100, 128, 256)])
+@pytest.mark.parametrize("rows,i_c,k_c", SIZES + [(5000, 40, 24), (9001, 33, 130), (4100, 128, 256),
+                                                        (2000, 300, 301), (1134, 374, 112), (700, 130, 1001)])
 def test_linear_grad(dtype, rows, i_c, k_c):
     for n, (act, gap) in enumerate([("none", 0), ("relu", 3), ("silu", 0), ("gelu", 8)]):
         g = torch.Generator().manual_seed(rows + i_c * 3 + k_c + n)
