@@ -645,7 +645,9 @@ def linear(X, K, bias=None, residual=None, act="none", residual_first=False, Y=N
         y_pitch = _activations(Y, "Y", k_c, dtype, device)
     if Z is not None:
         _dense(Z, shape, dtype, device, "Z")
-    workspace, nbytes = _scratch(linear_workspace_bytes(rows, i_c, k_c, dt), workspace, X)
+    nbytes = linear_workspace_bytes(rows, i_c, k_c, dt)
+    if nbytes:
+        workspace, nbytes = _scratch(nbytes, workspace, X)
     _on_device(X, "X")
     _launch("mec_linear", device, X.data_ptr(), K.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(),
             _ptr(Z), rows, i_c, k_c, x_pitch, r_pitch, y_pitch, dt, a, 1 if residual_first else 0,

@@ -357,17 +357,24 @@ constexpr int32_t kMaxShares = 64;  // of a product's reduction
 // the sums of a product's shares
 int64_t parts_bytes(const mec::ProductPlan& plan, int64_t M, int64_t N) { return plan.splits > 1 ? plan.splits * M * N * 4 : 0; }
 
-int64_t linear_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
-    return parts_bytes(mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares), rows, k_c);
+mec::ProductPlan linear_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
+    return mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares);
 }
 
-int64_t linear_grad_bytes(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
-    const int64_t dx = parts_bytes(mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares), rows, i_c);
-    const int64_t dk = parts_bytes(mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares), i_c, k_c);
-    const int64_t pair = parts_bytes(mec::plan_pair(dtype, rows, i_c, k_c, kMaxShares), i_c, k_c);
+// What a backward pass does by its sizes, and the workspace for it.
+struct GradPlan {
+    mec::ProductPlan x, k, pair;
+    int64_t bytes;
+};
+GradPlan grad_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
+    GradPlan g;
+    g.x = mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares);
+    g.k = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares);
+    g.pair = mec::plan_pair(g.x, g.k, dtype, rows, i_c, k_c, kMaxShares);
     const int64_t shares = mec::act_grad_shares(rows, k_c);  // one share goes straight to dbias
-    const int64_t db = shares > 1 ? shares * k_c * 4 : 0;
-    return std::max({dx, dk, pair, db});
+    g.bytes = std::max({parts_bytes(g.x, rows, i_c), parts_bytes(g.k, i_c, k_c), parts_bytes(g.pair, i_c, k_c),
+                        shares > 1 ? shares * k_c * 4 : int64_t(0)});
+    return g;
 }
 
 }  // namespace
@@ -382,7 +389,8 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     const int64_t es = elem_bytes(dtype);
     if (!aligned(X, es) || !aligned(K, es) || !aligned(bias, 4) || !aligned(R, es) || !aligned(Y, es) || !aligned(Z, es))
         return MEC_ERR_ALIGNMENT;
-    const int64_t need = linear_bytes(rows, i_c, k_c, dtype);
+    const mec::ProductPlan plan = linear_plan(rows, i_c, k_c, dtype);
+    const int64_t need = parts_bytes(plan, rows, k_c);
     if (need && (!workspace || (uint64_t)workspace_bytes < (uint64_t)need)) return MEC_ERR_WORKSPACE;
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     mec::Product p{};
@@ -405,22 +413,22 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     p.batch = 1;
     p.part = static_cast<float*>(workspace);
     clear_stale_error();
-    const mec::ProductPlan plan = mec::plan_product(mec::Layout::kXK, dtype, p, kMaxShares);
-    return hip_status(launch_shared(plan, mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
+    return hip_status(launch_shared(mec::refine_plan(plan, mec::Layout::kXK, dtype, p), mec::Layout::kXK, p, dtype,
+                                    (hipStream_t)stream), "linear");
 }
 
 int64_t mec_linear_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
     const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
     if (rc != MEC_OK) return rc;
     if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
-    return linear_bytes(rows, i_c, k_c, dtype);
+    return parts_bytes(linear_plan(rows, i_c, k_c, dtype), rows, k_c);
 }
 
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
     const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
     if (rc != MEC_OK) return rc;
     if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
-    return linear_grad_bytes(rows, i_c, k_c, dtype);
+    return grad_plan(rows, i_c, k_c, dtype).bytes;
 }
 
 int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX, void* dK, float* dbias,
@@ -434,10 +442,9 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     if (!aligned(G, es) || !aligned(X, es) || !aligned(K, es) || !aligned(Z, es) || !aligned(dZ, es) || !aligned(dX, es) ||
         !aligned(dK, es) || !aligned(dbias, 4))
         return MEC_ERR_ALIGNMENT;
-    if (dX || dK || dbias) {
-        const int64_t need = linear_grad_bytes(rows, i_c, k_c, dtype);
-        if (need && (!workspace || (uint64_t)workspace_bytes < (uint64_t)need)) return MEC_ERR_WORKSPACE;
-    }
+    const GradPlan plan = grad_plan(rows, i_c, k_c, dtype);
+    if ((dX || dK || dbias) && plan.bytes && (!workspace || (uint64_t)workspace_bytes < (uint64_t)plan.bytes))
+        return MEC_ERR_WORKSPACE;
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     const hipStream_t st = (hipStream_t)stream;
     float* const part = static_cast<float*>(workspace);
@@ -472,19 +479,16 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     k.K = (int32_t)rows;
     k.part = part;
     x.part = part;
-    const mec::ProductPlan px = mec::plan_product(mec::Layout::kXKt, dtype, x, kMaxShares);
-    const mec::ProductPlan pk = mec::plan_product(mec::Layout::kXtK, dtype, k, kMaxShares);
+    const mec::ProductPlan px = mec::refine_plan(plan.x, mec::Layout::kXKt, dtype, x);
+    const mec::ProductPlan pk = mec::refine_plan(plan.k, mec::Layout::kXtK, dtype, k);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
-    if (dX && dK) {
-        const mec::ProductPlan pair = mec::plan_pair(dtype, rows, i_c, k_c, kMaxShares);
-        if (pair.kernel) {
-            k.splits = pair.splits;
-            rc = hip_status(mec::launch_product_f32_pair(x, k, st), "gradients of the input and the kernel");
-            if (rc == MEC_OK && k.splits > 1)
-                rc = hip_status(mec::launch_sum_parts(part, k.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
-            return rc;
-        }
+    if (dX && dK && plan.pair.kernel) {
+        k.splits = plan.pair.splits;
+        rc = hip_status(mec::launch_product_f32_pair(x, k, st), "gradients of the input and the kernel");
+        if (rc == MEC_OK && k.splits > 1)
+            rc = hip_status(mec::launch_sum_parts(part, k.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
+        return rc;
     }
     if (dX) {
         rc = hip_status(launch_shared(px, mec::Layout::kXKt, x, dtype, st), "gradient of the input");

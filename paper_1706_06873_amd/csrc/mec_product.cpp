@@ -92,14 +92,14 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     return best;
 }
 
-ProductPlan plan_pair(int dtype, int64_t rows, int64_t i_c, int64_t k_c, int32_t max_splits) {
+ProductPlan plan_pair(const ProductPlan& px, const ProductPlan& pk, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
+                      int32_t max_splits) {
     ProductPlan best{0, 1, 0.0};
     if (dtype) return best;
     // what two launches take, by their models and a launch's own 3 us; the model of the pair is a
     // little too high (1000 x 1000 x 1000 49 where it took 44, two launches 50; 4608 x 256 x 1024
     // 57, 53 and 62; 20000 x 256 x 1024 166, 177 and 160; 11679 x 920 x 1619 508, 549 and 467)
-    best.us = 3.0 + 1.05 * (plan_product(Layout::kXKt, dtype, rows, i_c, k_c, 1, max_splits).us +
-                            plan_product(Layout::kXtK, dtype, i_c, k_c, rows, 1, max_splits).us);
+    best.us = 3.0 + 1.05 * (px.us + pk.us);
     const TileCost& t = kF32[kSymmetricF32 - 1];
     const int64_t nx = ceil_div(rows, t.tm) * ceil_div(i_c, t.tn), nk = ceil_div(i_c, t.tm) * ceil_div(k_c, t.tn);
     const int64_t shares = ceil_div(rows, 64);
@@ -124,8 +124,7 @@ bool clean_rows(Layout layout, const Product& p) {
     return rows16(p.A, p.lda) && rows16(p.B, p.ldb) && a_run % 8 == 0 && b_run % 8 == 0;
 }
 
-ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits) {
-    const ProductPlan plan = plan_product(layout, dtype, p.M, p.N, p.K, 1, max_splits);
+ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const Product& p) {
     const Operands with{!dtype || clean_rows(layout, p), p.R != nullptr, p.Z != nullptr};
     return with.clean && !with.R && !with.Z ? plan : plan_product(layout, dtype, p.M, p.N, p.K, 1, plan.splits, false, with);
 }

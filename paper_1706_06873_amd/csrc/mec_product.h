@@ -56,11 +56,12 @@ struct Operands {
 // max_splits: as many shares as the caller has room for partial sums (batch x M x N each)
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
                          bool symmetric = false, const Operands& with = {});
-// one product on its operands as they lie, in no more shares than the first takes by the sizes alone
-ProductPlan plan_product(Layout layout, int dtype, const Product& p, int32_t max_splits);
+// the plan by the sizes alone, for the operands as they are: in no more shares
+ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const Product& p);
 // dX (rows x i_c) and dK (i_c x k_c) of fp32 by tiles in one launch: kernel 3 and dK's shares, or
-// kernel 0 where two launches are as fast
-ProductPlan plan_pair(int dtype, int64_t rows, int64_t i_c, int64_t k_c, int32_t max_splits);
+// kernel 0 where two launches by those plans are as fast
+ProductPlan plan_pair(const ProductPlan& x, const ProductPlan& k, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
+                      int32_t max_splits);
 // A's and B's rows are whole 16-byte granules (bf16)
 bool clean_rows(Layout layout, const Product& p);
 
