@@ -483,9 +483,11 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     const mec::ProductPlan pk = mec::refine_plan(plan.k, mec::Layout::kXtK, dtype, k);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
-    if (dX && dK && plan.pair.kernel) {
+    if (dX && dK && plan.pair.kernel &&
+        (!dtype || (mec::clean_rows(mec::Layout::kXKt, x) && mec::clean_rows(mec::Layout::kXtK, k)))) {
         k.splits = plan.pair.splits;
-        rc = hip_status(mec::launch_product_f32_pair(x, k, st), "gradients of the input and the kernel");
+        rc = hip_status(dtype ? mec::launch_product_bf16_pair(x, k, st) : mec::launch_product_f32_pair(x, k, st),
+                        "gradients of the input and the kernel");
         if (rc == MEC_OK && k.splits > 1)
             rc = hip_status(mec::launch_sum_parts(part, k.splits, (int64_t)i_c * k_c, dK, dtype, st), "sum of the kernel's gradient");
         return rc;

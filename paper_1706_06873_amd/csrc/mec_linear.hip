@@ -183,16 +183,15 @@ struct Operand {
     }
 };
 
+// Workgroup b's tile, in C::LDS bytes of LDS.
 template <class C>
-__global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
+__device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
     constexpr int BM = C::kBM, BN = C::kBN, KT = C::kKT;
     using OpA = Operand<C::TM, C::THREADS, C::kKT, C::kAT, C::kDMA>;
     using OpB = Operand<C::TN, C::THREADS, C::kKT, C::kBT, C::kDMA>;
-    __shared__ __align__(16) char lds[C::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform((uint32_t)tid >> 6);
     const int wm = wave % C::kWM, wn = wave / C::kWM;
     const uint32_t tiles = (uint32_t)p.m_tiles * (uint32_t)p.n_tiles;
-    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
     const uint32_t split = b / tiles;
     uint32_t mt, nt;
     tile_of(b - split * tiles, (uint32_t)p.m_tiles, (uint32_t)p.n_tiles, 8u, mt, nt);
@@ -319,21 +318,44 @@ __global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
     epilogue<uint16_t, BM, BN>(p, acc, mine, m0 + wm * BM * 32, n0 + wn * BN * 32, 0, (int32_t)split, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int KT, int S, Layout L>
-hipError_t run(Product p, hipStream_t stream) {
-    using C = Cfg<BM, BN, WM, WN, KT, S, L, true>;
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void product_bf16_kernel(Product p) {
+    __shared__ __align__(16) char lds[C::LDS];
+    product_bf16<C>(p, xcd_remap(blockIdx.x, gridDim.x), lds);
+}
+
+// The two products of a backward pass in one launch, as in fp32.
+template <class X, class K>
+__global__ __launch_bounds__(X::THREADS) void product_bf16_pair_kernel(Product x, Product k, uint32_t x_blocks) {
+    static_assert(X::LDS == K::LDS && X::THREADS == K::THREADS, "one shape of tiles");
+    __shared__ __align__(16) char lds[X::LDS];
+    if (blockIdx.x < x_blocks) product_bf16<X>(x, xcd_remap(blockIdx.x, x_blocks), lds);
+    else product_bf16<K>(k, xcd_remap(blockIdx.x - x_blocks, gridDim.x - x_blocks), lds);
+}
+
+// Fills what the kernels need; the workgroups, or 0 past the grid or for shares that leave some empty.
+template <class C>
+uint32_t prepare(Product& p) {
+    constexpr int KT = C::kKT;
     p.m_tiles = (p.M + C::TM - 1) / C::TM;
     p.n_tiles = (p.N + C::TN - 1) / C::TN;
     // shares are whole multiples of 64 elements
     const int64_t chunks = 64 / KT * (((int64_t)p.K + 63) / 64);
     p.chunks = 64 / KT * (int32_t)((chunks / (64 / KT) + p.splits - 1) / p.splits);
     const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * p.splits;
-    if (blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks) return hipErrorInvalidValue;
+    return blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
+}
+
+template <int BM, int BN, int WM, int WN, int KT, int S, Layout L>
+hipError_t run(Product p, hipStream_t stream) {
+    using C = Cfg<BM, BN, WM, WN, KT, S, L, true>;
+    const uint32_t blocks = prepare<C>(p);
+    if (!blocks) return hipErrorInvalidValue;
     if (p.clean) {
-        hipLaunchKernelGGL(product_bf16_kernel<C>, dim3((uint32_t)blocks), dim3(C::THREADS), 0, stream, p);
+        hipLaunchKernelGGL(product_bf16_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, stream, p);
     } else {
         using G = Cfg<BM, BN, WM, WN, KT, 2, L, false>;
-        hipLaunchKernelGGL(product_bf16_kernel<G>, dim3((uint32_t)blocks), dim3(G::THREADS), 0, stream, p);
+        hipLaunchKernelGGL(product_bf16_kernel<G>, dim3(blocks), dim3(G::THREADS), 0, stream, p);
     }
     return hipGetLastError();
 }
@@ -351,6 +373,16 @@ hipError_t pick(const Product& p, int tile, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_product_bf16_pair(Product x, Product k, hipStream_t stream) {
+    using X = Cfg<1, 2, 2, 2, 64, 2, Layout::kXKt, true>;
+    using K = Cfg<1, 2, 2, 2, 64, 2, Layout::kXtK, true>;
+    if (!clean_rows(Layout::kXKt, x) || !clean_rows(Layout::kXtK, k)) return hipErrorInvalidValue;
+    const uint32_t bx = prepare<X>(x), bk = prepare<K>(k);
+    if (!bx || !bk || bx > 0x7fffffffu - bk) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((product_bf16_pair_kernel<X, K>), dim3(bx + bk), dim3(X::THREADS), 0, stream, x, k, bx);
+    return hipGetLastError();
+}
 
 hipError_t launch_product_bf16(Layout layout, Product p, int tile, hipStream_t stream) {
     p.clean = clean_rows(layout, p);

@@ -37,6 +37,7 @@ constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 4.8, 0.9, 3.2},
                              {64, 64, 3, {0.64, 0.95, 1.15}, 5.0, 1.0, 2.5},
                              {64, 64, 1, {0.48}, 7.0, 1.0, 2.5}};
 
+constexpr int kPair = 3;          // the kernel whose tiles a pair of products takes
 constexpr int kSymmetricF32 = 3;  // the fp32 kernels from this one on have square tiles
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -95,24 +96,25 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
 ProductPlan plan_pair(const ProductPlan& px, const ProductPlan& pk, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
                       int32_t max_splits) {
     ProductPlan best{0, 1, 0.0};
-    if (dtype) return best;
-    // what two launches take, by their models and a launch's own 3 us; the model of the pair is a
+    // What two launches take, by their models and a launch's own 3 us; the model of the pair is a
     // little too high (1000 x 1000 x 1000 49 where it took 44, two launches 50; 4608 x 256 x 1024
-    // 57, 53 and 62; 20000 x 256 x 1024 166, 177 and 160; 11679 x 920 x 1619 508, 549 and 467)
+    // 57, 53 and 62; 20000 x 256 x 1024 166, 177 and 160; 11679 x 920 x 1619 508, 549 and 467;
+    // bf16 2447 x 872 x 2144 40 and 60, 6272 x 1024 x 256 28 and 34, but 800 x 512 x 2048 27 and 24).
     best.us = 3.0 + 1.05 * (px.us + pk.us);
-    const TileCost& t = kF32[kSymmetricF32 - 1];
+    const TileCost& t = (dtype ? kBf16 : kF32)[kPair - 1];
+    const int64_t step = dtype ? 64 : 32;
     const int64_t nx = ceil_div(rows, t.tm) * ceil_div(i_c, t.tn), nk = ceil_div(i_c, t.tm) * ceil_div(k_c, t.tn);
     const int64_t shares = ceil_div(rows, 64);
     auto tile = [&](int64_t chunks) { return (double)chunks * t.chunk[t.fit - 1] + t.ends; };
     for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
         if (s > 1 && (shares < 4 * s || s * i_c * k_c > (int64_t(1) << 26))) break;
         const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
-        const double x = tile(ceil_div(k_c, 32)), k = tile(real > 1 ? 2 * per : ceil_div(rows, 32));
+        const double x = tile(ceil_div(k_c, step)), k = tile(real > 1 ? per * 64 / step : ceil_div(rows, step));
         // the compute units are full but for the last tile's time
         double us = ((double)nx * x + (double)(nk * real) * k) / (256.0 * t.fit);
         us += 0.5 * (x > k ? x : k);
         if (real > 1) us += 3.0 + (double)(real * i_c * k_c) / 1.2e6;
-        if (us < best.us) best = {kSymmetricF32, (int32_t)real, us};
+        if (us < best.us) best = {kPair, (int32_t)real, us};
     }
     return best;
 }

@@ -58,7 +58,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
                          bool symmetric = false, const Operands& with = {});
 // the plan by the sizes alone, for the operands as they are: in no more shares
 ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const Product& p);
-// dX (rows x i_c) and dK (i_c x k_c) of fp32 by tiles in one launch: kernel 3 and dK's shares, or
+// dX (rows x i_c) and dK (i_c x k_c) by tiles in one launch: kernel 3 and dK's shares, or
 // kernel 0 where two launches by those plans are as fast
 ProductPlan plan_pair(const ProductPlan& x, const ProductPlan& k, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
                       int32_t max_splits);
@@ -83,8 +83,9 @@ struct OrthStep {
 };
 hipError_t launch_orth_step(const OrthStep& p, int32_t batch, hipStream_t stream);
 // the two products of a backward pass, x of layout kXKt (in one share) and k of kXtK, in one launch:
-// by 64 x 64 tiles, or both small
+// by 64 x 64 tiles, 64 x 128 tiles (clean rows), or both small
 hipError_t launch_product_f32_pair(Product x, Product k, hipStream_t stream);
+hipError_t launch_product_bf16_pair(Product x, Product k, hipStream_t stream);
 hipError_t launch_product_small_pair(Product x, Product k, int dtype, hipStream_t stream);
 // by the plan, in one share
 hipError_t launch_product(Layout layout, const Product& p, int dtype, hipStream_t stream);
