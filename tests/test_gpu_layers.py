@@ -506,6 +506,38 @@ def test_block_captured_in_a_graph():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_shared_and_paired_products_captured(dtype):
+    """Products in shares, the two of a backward pass in one launch and a stack's update, in a
+    graph that is replayed between eager calls of the same on other inputs."""
+    g = torch.Generator().manual_seed(13)
+    inputs = [[randn(g, *s).to(dtype).to(DEV) for s in ((512, 9000), (9000, 64), (2000, 296), (296, 304), (2000, 304), (3, 700, 160))]
+              for _ in range(3)]
+
+    def work(X, K, X2, K2, G, U):
+        Z = torch.empty_like(G)
+        H = mec.linear(X2, K2, act="gelu", Z=Z)
+        return (mec.linear(X, K, act="silu"), H, *mec.linear_grad(G, X2, K2, Z, "gelu"), mec.orthogonalize(U))
+
+    fixed = [t.clone() for t in inputs[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work(*fixed)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = work(*fixed)
+    for given in inputs[::-1]:
+        want = work(*given)
+        for t, v in zip(fixed, given):
+            t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
 def test_streams_and_repeatability():
     """The same bits every time, also from two streams at once with workspaces of their own."""
     g = torch.Generator().manual_seed(21)
