@@ -200,6 +200,36 @@ def test_linear_spreads_infinities_and_nans_as_the_formula(dtype, rows, i_c, k_c
     assert torch.allclose(Y[~odd].float(), ok[~odd].float(), rtol=2.0 ** -7, atol=1e-4)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_shared_and_paired_products_spread_infinities_and_nans(dtype):
+    """The same where workgroups or waves share a reduction, and where two products share a launch."""
+    g = torch.Generator().manual_seed(10)
+
+    def check(got, want, size):
+        got = got.cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        ok = torch.isfinite(want)
+        tol = size + HALF[dtype] * (want.abs() + size)
+        assert ((got.double() - want).abs()[ok] <= tol[ok]).all()
+
+    def product(a, b):  # (finite magnitudes for the bound)
+        m = lambda t: torch.nan_to_num(t.double().abs(), 0.0, 0.0, 0.0)  # noqa: E731
+        return a.double() @ b.double(), (a.shape[1] + 8) * 2.0 ** -23 * (m(a) @ m(b))
+
+    for rows, i_c, k_c in [(512, 9000, 64), (600, 4100, 1000)]:
+        X, K = randn(g, rows, i_c).to(dtype), randn(g, i_c, k_c).to(dtype)
+        X[1, i_c - 1], X[3, 0], K[2, 4], X[rows - 1, i_c // 2] = math.inf, math.nan, -math.inf, -math.inf
+        print("[case]", dtype, rows, i_c, k_c, flush=True)
+        check(mec.linear(X.to(DEV), K.to(DEV)), *product(X, K))
+    rows, i_c, k_c = 2000, 296, 304
+    X, K, G = randn(g, rows, i_c).to(dtype), randn(g, i_c, k_c).to(dtype), randn(g, rows, k_c).to(dtype)
+    X[5, 7], G[70, 300], G[1999, 0] = math.inf, math.nan, -math.inf
+    dX, dK, db, _ = mec.linear_grad(G.to(DEV), X.to(DEV), K.to(DEV))
+    check(dX, *product(G, K.T))
+    check(dK, *product(X.T, G))
+    assert torch.isnan(db[300]) and db[0] == -math.inf and torch.isfinite(db[1:300]).all()
+
+
 def test_linear_far_values_fp32():
     """Values at the ends of fp32's range: what the split into bf16 parts does not hold."""
     g = torch.Generator().manual_seed(10)
