@@ -315,8 +315,8 @@ int mec_conv2d_wgrad_noalloc(const void* I, const float* G, float* dK,
  * gamma, beta, their gradients and the row statistics are fp32, and so is
  * everything between: each output is rounded once. Widths and pitches go up to
  * 2^20, rows to 2^30 (MEC_ERR_UNSUPPORTED beyond). Results are reproducible:
- * every sum has an order fixed by the sizes, the alignments and which operands
- * are given (no atomics).
+ * every sum has an order fixed by the sizes, the alignments, the activation and which
+ * operands are given (no atomics).
  * Infinities and NaNs spread as in the formulas.
  * ------------------------------------------------------------------------ */
 
@@ -346,11 +346,13 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
  * R is dZ where residual_first, else G. dZ and dX are dense, as Z is. dX, dK and
  * dbias may each be NULL: not wanted (X is then read for dK, K for dX alone). With
  * MEC_ACT_NONE dZ is G: Z and dZ may be NULL and are not touched; otherwise dZ is
- * always written, and products take it as rounded to dtype; it may be Z's memory,
- * or G's where g_pitch = k_c. Otherwise outputs must overlap neither each other nor
- * the inputs.
- * workspace: mec_linear_grad_workspace_bytes, 4-byte aligned, for partial sums; may be NULL
- * where that is 0 or none of dX, dK and dbias is wanted. */
+ * always written; it may be Z's memory, or G's where g_pitch = k_c. Otherwise outputs must
+ * overlap neither each other nor the inputs. dX and dK are not the products of dZ as rounded
+ * to bf16: they take it with 16 significant bits (fp32: with all of them).
+ * workspace: mec_linear_grad_act_workspace_bytes, 4-byte aligned, for partial sums and for what
+ * rounding dZ to bf16 leaves over; may be NULL where that is 0 or none of dX, dK and dbias is
+ * wanted. mec_linear_grad_workspace_bytes is enough for every activation. */
+int64_t mec_linear_grad_act_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype, int act);
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype);
 int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX,
                     void* dK, float* dbias, void* workspace, size_t workspace_bytes, int64_t rows,

@@ -83,6 +83,8 @@ def _load(path):
     L.mec_linear.argtypes = [_vp] * 6 + [i64, _i, _i, i64, i64, i64, _i, _i, _i, _vp, sz, _vp]
     L.mec_linear_workspace_bytes.argtypes = [i64, _i, _i, _i]
     L.mec_linear_grad_workspace_bytes.argtypes = [i64, _i, _i, _i]
+    L.mec_linear_grad_act_workspace_bytes.argtypes = [i64, _i, _i, _i, _i]
+    L.mec_linear_grad_act_workspace_bytes.restype = i64
     L.mec_linear_grad.argtypes = [_vp] * 9 + [sz, i64, _i, _i, i64, i64, _i, _i, _vp]
     L.mec_layer_norm.argtypes = [_vp] * 6 + [i64, _i, i64, i64, f, _i, _vp]
     L.mec_layer_norm_grad_workspace_bytes.argtypes = [i64, _i, _i]
@@ -661,7 +663,11 @@ def linear_workspace_bytes(rows, i_c, k_c, dtype=F32):
 
 
 @functools.lru_cache(4096)
-def linear_grad_workspace_bytes(rows, i_c, k_c, dtype=F32):
+def linear_grad_workspace_bytes(rows, i_c, k_c, dtype=F32, act=None):
+    """For calls with this activation; without one, enough for calls with any."""
+    if act is not None:
+        return _check(lib.mec_linear_grad_act_workspace_bytes(rows, i_c, k_c, dtype, _act_code(act)),
+                      "mec_linear_grad_act_workspace_bytes")
     return _check(lib.mec_linear_grad_workspace_bytes(rows, i_c, k_c, dtype), "mec_linear_grad_workspace_bytes")
 
 
@@ -671,8 +677,8 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     (not needed with act "none"); `needs` says which of dX, dK and dbias are wanted, the
     others come back as None (X may be None without dK). dZ, the gradient of act's argument, is G
     itself with act "none"; the residual's gradient is dZ where it was added first, else G.
-    dK has K's dtype and shape, dbias is float32. A given workspace holds at least
-    linear_grad_workspace_bytes bytes."""
+    dK has K's dtype and shape, dbias is float32; none of the three is computed from dZ as rounded
+    to bfloat16. A given workspace holds at least linear_grad_workspace_bytes bytes."""
     if stream is not None:
         return _on(stream, linear_grad, G, X, K, Z, act, needs, dZ, dX, dK, dbias, workspace)
     gs, rows, k_c, dt = _channels(G, "G")
@@ -702,7 +708,7 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     dbias = _new(dbias, (k_c,), _F32, G, "dbias") if need_b else None
     nbytes = 0
     if need_x or need_k or need_b:
-        workspace, nbytes = _scratch(linear_grad_workspace_bytes(rows, i_c, k_c, dt), workspace, G)
+        workspace, nbytes = _scratch(linear_grad_workspace_bytes(rows, i_c, k_c, dt, act), workspace, G)
     _on_device(G, "G")
     _launch("mec_linear_grad", device, G.data_ptr(), _ptr(X), K.data_ptr(), _ptr(Z), _ptr(dZ) if a else None, _ptr(dX),
             _ptr(dK), _ptr(dbias), _ptr(workspace) if nbytes else None, nbytes, rows, i_c, k_c, g_pitch, x_pitch, dt, a)

@@ -361,19 +361,26 @@ mec::ProductPlan linear_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype) 
     return mec::plan_product(mec::Layout::kXK, dtype, rows, k_c, i_c, 1, kMaxShares);
 }
 
-// What a backward pass does by its sizes, and the workspace for it.
+// What a backward pass does by its sizes and activation, and the workspace for it: partial sums
+// and, 16-byte aligned behind them, dZ's second part where there is one. (ReLU's dZ is G or 0, so
+// that rounding it leaves nothing over.)
 struct GradPlan {
     mec::ProductPlan x, k, pair;
-    int64_t bytes;
+    int64_t sums, bytes;
+    bool two;
 };
-GradPlan grad_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype) {
+GradPlan grad_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype, int act) {
     GradPlan g;
-    g.x = mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares);
-    g.k = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares);
-    g.pair = mec::plan_pair(g.x, g.k, dtype, rows, i_c, k_c, kMaxShares);
+    g.two = dtype == MEC_BF16 && act > MEC_ACT_RELU;
+    mec::Operands with;
+    with.two = g.two;
+    g.x = mec::plan_product(mec::Layout::kXKt, dtype, rows, i_c, k_c, 1, kMaxShares, false, with);
+    g.k = mec::plan_product(mec::Layout::kXtK, dtype, i_c, k_c, rows, 1, kMaxShares, false, with);
+    g.pair = mec::plan_pair(g.x, g.k, dtype, rows, i_c, k_c, kMaxShares, g.two);
     const int64_t shares = mec::act_grad_shares(rows, k_c);  // one share goes straight to dbias
-    g.bytes = std::max({parts_bytes(g.x, rows, i_c), parts_bytes(g.k, i_c, k_c), parts_bytes(g.pair, i_c, k_c),
-                        shares > 1 ? shares * k_c * 4 : int64_t(0)});
+    g.sums = std::max({parts_bytes(g.x, rows, i_c), parts_bytes(g.k, i_c, k_c), parts_bytes(g.pair, i_c, k_c),
+                       shares > 1 ? shares * k_c * 4 : int64_t(0)});
+    g.bytes = g.sums + (g.two ? 16 + 2 * rows * k_c : 0);
     return g;
 }
 
@@ -428,7 +435,14 @@ int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtyp
     const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
     if (rc != MEC_OK) return rc;
     if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
-    return grad_plan(rows, i_c, k_c, dtype).bytes;
+    return std::max(grad_plan(rows, i_c, k_c, dtype, MEC_ACT_NONE).bytes, grad_plan(rows, i_c, k_c, dtype, MEC_ACT_GELU).bytes);
+}
+
+int64_t mec_linear_grad_act_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype, int act) {
+    const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
+    if (rc != MEC_OK) return rc;
+    if (!valid_dtype(dtype) || !valid_act(act)) return MEC_ERR_INVALID_ARG;
+    return grad_plan(rows, i_c, k_c, dtype, act).bytes;
 }
 
 int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, void* dZ, void* dX, void* dK, float* dbias,
@@ -442,16 +456,17 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     if (!aligned(G, es) || !aligned(X, es) || !aligned(K, es) || !aligned(Z, es) || !aligned(dZ, es) || !aligned(dX, es) ||
         !aligned(dK, es) || !aligned(dbias, 4))
         return MEC_ERR_ALIGNMENT;
-    const GradPlan plan = grad_plan(rows, i_c, k_c, dtype);
+    const GradPlan plan = grad_plan(rows, i_c, k_c, dtype, act);
     if ((dX || dK || dbias) && plan.bytes && (!workspace || (uint64_t)workspace_bytes < (uint64_t)plan.bytes))
         return MEC_ERR_WORKSPACE;
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
     const hipStream_t st = (hipStream_t)stream;
     float* const part = static_cast<float*>(workspace);
+    char* const low = plan.two && (dX || dK) ? reinterpret_cast<char*>(((uintptr_t)workspace + plan.sums + 15) / 16 * 16) : nullptr;
     clear_stale_error();
     if (act != MEC_ACT_NONE || dbias) {
-        rc = hip_status(mec::launch_act_grad(G, g_pitch, Z, act == MEC_ACT_NONE ? nullptr : dZ, dbias, part, rows, k_c, act,
-                                             dtype, st), "gradients of the activation and the bias");
+        rc = hip_status(mec::launch_act_grad(G, g_pitch, Z, act == MEC_ACT_NONE ? nullptr : dZ, low, dbias, part, rows, k_c,
+                                             act, dtype, st), "gradients of the activation and the bias");
         if (rc != MEC_OK) return rc;
     }
     const void* const dz = act == MEC_ACT_NONE ? G : dZ;
@@ -479,6 +494,7 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     k.K = (int32_t)rows;
     k.part = part;
     x.part = part;
+    x.second = k.second = low ? (int64_t)((uintptr_t)low - (uintptr_t)dZ) : 0;
     const mec::ProductPlan px = mec::refine_plan(plan.x, mec::Layout::kXKt, dtype, x);
     const mec::ProductPlan pk = mec::refine_plan(plan.k, mec::Layout::kXtK, dtype, k);
     if (dX && dK && px.kernel == 0 && pk.kernel == 0)
@@ -628,6 +644,46 @@ int mec_internal_wgrad(int kernel, const void* A, const float* G, float* dK, voi
     return hip_status(mec::launch_wgrad_by((mec::WgradKernel)kernel, s, static_cast<const float*>(A), G,
                                            static_cast<float*>(workspace), dK, (hipStream_t)stream, fused),
                       "one kernel's wgrad products");
+}
+
+int mec_internal_product_with(int kernel, int layout, int dtype, int M, int N, int K, const mec_internal_operands* o, void* stream) {
+    if (layout < 0 || layout > 2 || !valid_dtype(dtype) || !o || !o->A || !o->B || !o->Y || M < 1 || N < 1 || K < 1 ||
+        o->splits < 1 || (o->splits > 1 && !o->part) || o->batch < 1 || !valid_act(o->act))
+        return MEC_ERR_INVALID_ARG;
+    mec::Product p{};
+    p.A = o->A;
+    p.B = o->B;
+    p.Y = o->Y;
+    p.Z = o->Z;
+    p.R = o->R;
+    p.bias = o->bias;
+    p.part = o->part;
+    p.lda = o->lda;
+    p.ldb = o->ldb;
+    p.ldy = o->ldy;
+    p.ldz = o->ldz;
+    p.ldr = o->ldr;
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    p.act = o->act;
+    p.res_first = o->res_first;
+    p.alpha = o->alpha;
+    p.beta = o->beta;
+    p.diag = o->diag;
+    p.batch = o->batch;
+    p.a_batch = o->a_batch;
+    p.b_batch = o->b_batch;
+    p.y_batch = p.r_batch = (int64_t)M * o->ldy;
+    p.symmetric = o->symmetric;
+    p.second = o->second;
+    clear_stale_error();
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = mec::launch_product({kernel, o->splits, 0.0}, (mec::Layout)layout, p, dtype, st);
+    if (e == hipErrorNotSupported) return MEC_ERR_UNSUPPORTED;
+    const int rc = hip_status(e, "one kernel's product");
+    if (rc != MEC_OK || o->splits == 1) return rc;
+    return hip_status(mec::launch_sum_parts(o->part, o->splits, (int64_t)o->batch * M * N, o->Y, dtype, st), "sum");
 }
 
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {

@@ -240,6 +240,20 @@ extern "C" int mec_internal_product_plan(int layout, int dtype, int M, int N, in
 // 1 the tile kernels; Y's rows are dense where splits > 1 (part: splits x M x N floats).
 extern "C" int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits,
                                     int M, int N, int K, int64_t lda, int64_t ldb, int64_t ldy, int dtype, void* stream);
+// The same with all that a product may have (mec_product.h); the batch's outputs and residuals
+// M*ldy elements apart. With shares Y is the sum alone: no epilogue.
+struct mec_internal_operands {
+    const void *A, *B;
+    void *Y, *Z;
+    const void* R;
+    const float* bias;
+    float* part;
+    int64_t lda, ldb, ldy, ldz, ldr, a_batch, b_batch, second;
+    int splits, batch, act, res_first, symmetric;
+    float alpha, beta, diag;
+};
+extern "C" int mec_internal_product_with(int kernel, int layout, int dtype, int M, int N, int K, const mec_internal_operands* o,
+                                         void* stream);
 
 #if defined(__HIP__)
 namespace mec {

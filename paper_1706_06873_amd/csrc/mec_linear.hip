@@ -12,6 +12,10 @@
 // Both orders put the lanes that read together on different banks. Rows of whole 16-byte
 // granules go straight to LDS (buffer_load .. lds; what lies past the end of the reduction
 // is past the resource's end and arrives as zeros); others go through registers.
+//
+// dZ of the two gradients may come as two matrices whose sum it is (Product::second): chunks
+// of the one and of the other take turns, against the same chunk of the other operand, so
+// that dX and dK are as from dZ in 16 significant bits, at twice the products.
 #include "mec_product.h"
 #include "mec_split.h"
 
@@ -26,6 +30,7 @@ struct Cfg {
     static constexpr bool kAT = L == Layout::kXtK;   // A stored [k][m]
     static constexpr bool kBT = L != Layout::kXKt;   // B stored [k][n]
     static constexpr bool kDMA = DMA;
+    static constexpr bool kGrad = L != Layout::kXK;  // dZ, A of dX and B of dK, may come in two parts
     static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int AB = TM * kKT * 2, BB = TN * kKT * 2, STAGE = AB + BB;  // bytes
     static constexpr int kLoads = (TM + TN) * (KT / 8) / THREADS;                // granules per thread
@@ -116,9 +121,10 @@ struct Operand {
             }
         }
     }
-    __device__ inline void next() {
-        base += step;
-        left -= TR && DMA ? step : KT;
+    // To the next chunk, or (on false) not along the reduction, and `jump` bytes to dZ's other part.
+    __device__ inline void next(bool on, int64_t jump) {
+        base += (on ? step : 0) + jump;
+        left -= on ? (TR && DMA ? step : KT) : 0;
     }
     // DMA: this chunk to LDS at `to`
     __device__ inline void stage(uint32_t to, int wave) const {
@@ -198,7 +204,8 @@ __device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
     const int32_t m0 = (int32_t)mt * C::TM, n0 = (int32_t)nt * C::TN;
     const int64_t k0 = (int64_t)split * p.chunks * KT;
     const int64_t k1 = k0 + (int64_t)p.chunks * KT < p.K ? k0 + (int64_t)p.chunks * KT : p.K;
-    const int chunks = (int)((k1 - k0 + KT - 1) / KT);
+    const bool two = C::kGrad && p.second != 0;
+    const int chunks = (int)((k1 - k0 + KT - 1) / KT) << (two ? 1 : 0);
 
     OpA a;
     OpB bb;
@@ -230,11 +237,18 @@ __device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
             multiply(f);
         }
     };
+    bool on = !two;
+    int64_t jump = two ? p.second : 0;
+    auto next = [&] {
+        a.next(on, C::kAT ? 0 : jump);
+        bb.next(on, C::kAT ? jump : 0);
+        on = on != two;
+        jump = -jump;
+    };
     auto stage = [&](uint32_t to) {
         a.stage(at + to, wave);
         bb.stage(at + to + C::AB, wave);
-        a.next();
-        bb.next();
+        next();
     };
     if constexpr (C::kDMA && C::kS > 2) {
         // S - 1 chunks on their way; those past the last are zeros, so that the loads in
@@ -301,8 +315,7 @@ __device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
             __syncthreads();
             const bool more = c + 1 < chunks;
             if (more) {
-                a.next();
-                bb.next();
+                next();
                 a.load(ra);
                 bb.load(rb);
             }
@@ -311,6 +324,22 @@ __device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
                 OpA::put(ra, lds + then, tid);
                 OpB::put(rb, lds + then + C::AB, tid);
             }
+        }
+    }
+    if constexpr (C::kGrad) {
+        if (two) {
+            const uint16_t* const A = static_cast<const uint16_t*>(p.A) + k0 * (C::kAT ? p.lda : 1);
+            const uint16_t* const B = static_cast<const uint16_t*>(p.B) + k0 * (C::kBT ? p.ldb : 1);
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+#pragma unroll
+                for (int j = 0; j < BN; ++j) {
+                    int32_t m = m0 + (wm * BM + i) * 32 + (lane & 31), n = n0 + (wn * BN + j) * 32 + (lane & 31);
+                    m = m < p.M ? m : p.M - 1;
+                    n = n < p.N ? n : p.N - 1;
+                    finite_or_first(acc[i][j], A + m * (C::kAT ? 1 : p.lda), C::kAT ? p.lda : 1, B + n * (C::kBT ? 1 : p.ldb),
+                                    C::kBT ? p.ldb : 1, (int32_t)(k1 - k0), lane);
+                }
         }
     }
     __syncthreads();

@@ -1,5 +1,7 @@
 // What the gradients of the layer operators need beside their products: dZ = G act'(Z) with
-// the column sums of dZ, and the sums of partial sums.
+// the column sums of dZ, and the sums of partial sums. dZ in bf16 comes in two parts, the output
+// and what its rounding left over: the products take both, since the rounding of dZ alone (2^-8
+// at most) would weigh as much in dX and dK as the rounding of their own.
 //
 // act_grad_kernel is one pass over G and Z, bound by memory. A workgroup takes a strip of
 // columns and a share of the rows; a thread keeps the sums of its own columns in registers
@@ -14,6 +16,7 @@ struct ActGradParams {
     const void* G;
     const void* Z;
     void* dZ;     // or nullptr (then act is none)
+    void* low;    // dZ's second part, or nullptr
     float* part;  // shares x N, or nullptr
     int64_t ldg, rows, rows_per_share;
     int32_t N, act;
@@ -59,6 +62,13 @@ __global__ __launch_bounds__(THREADS) void act_grad_kernel(ActGradParams p) {
                     Pack8<E> o;
                     o.round(x);
                     o.store(static_cast<E*>(p.dZ) + (r + u * TY) * p.N + n, have);
+                    if (p.low) {
+                        float y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = __builtin_isfinite(o.get(e)) ? x[e] - o.get(e) : 0.0f;
+                        o.round(y);
+                        o.store(static_cast<E*>(p.low) + (r + u * TY) * p.N + n, have);
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += x[e];
@@ -250,13 +260,14 @@ int32_t act_grad_shares(int64_t rows, int64_t N) {
     return (int32_t)(shares < most ? shares : most);
 }
 
-hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* dbias, float* part, int64_t rows,
-                           int32_t N, int act, int dtype, hipStream_t stream) {
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, void* low, float* dbias, float* part,
+                           int64_t rows, int32_t N, int act, int dtype, hipStream_t stream) {
     const int32_t shares = act_grad_shares(rows, N);
     ActGradParams p{};
     p.G = G;
     p.Z = Z;
     p.dZ = dZ;
+    p.low = low;
     p.part = !dbias ? nullptr : shares == 1 ? dbias : part;
     p.ldg = ldg;
     p.rows = rows;

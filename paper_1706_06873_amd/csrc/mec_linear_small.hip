@@ -332,9 +332,15 @@ __device__ inline void small_bf16(const Product& p, uint32_t b0, char* lds) {
         char* const patch_a = patch_b + (BT ? kPatch : 0);
         Turn<AT, CLEAN> ta;
         Turn<BT, CLEAN> tb;
-        ta.load(a, p.lda, p.M - t.m0, t.k.k0, t.k.k1, lane);
-        tb.load(b, p.ldb, p.N - t.n0, t.k.k0, t.k.k1, lane);
-        for (int32_t k = t.k.k0; k < t.k.k1; k += kRun) {
+        // dZ (A of dX, B of dK) in two parts: turns of the one and of the other
+        const int64_t second = L != Layout::kXK ? p.second / 2 : 0;
+        auto load = [&](int32_t k, int64_t part) {
+            ta.load(a + (AT ? 0 : part), p.lda, p.M - t.m0, k, t.k.k1, lane);
+            tb.load(b + (AT ? part : 0), p.ldb, p.N - t.n0, k, t.k.k1, lane);
+        };
+        int64_t part = 0;
+        load(t.k.k0, part);
+        for (int32_t k = t.k.k0; k < t.k.k1;) {
             bf16x8 fa[4], fb[4];
             ta.put(patch_a, lane);
             tb.put(patch_b, lane);
@@ -347,16 +353,21 @@ __device__ inline void small_bf16(const Product& p, uint32_t b0, char* lds) {
                 fa[i] = ta.frag(patch_a, i, lane);
                 fb[i] = tb.frag(patch_b, i, lane);
             }
-            if (k + kRun < t.k.k1) {
-                ta.load(a, p.lda, p.M - t.m0, k + kRun, t.k.k1, lane);
-                tb.load(b, p.ldb, p.N - t.n0, k + kRun, t.k.k1, lane);
-            }
+            if (L == Layout::kXK || part == second) k += kRun;
+            if (L != Layout::kXK) part = second - part;
+            if (k < t.k.k1) load(k, part);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i], fa[i], acc, 0, 0, 0);
             if constexpr (AT || BT) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_wave_barrier();
             }
+        }
+        if (second) {
+            const int32_t m = (lane & 31) < p.M - t.m0 ? (lane & 31) : p.M - t.m0 - 1;
+            const int32_t n = (lane & 31) < p.N - t.n0 ? (lane & 31) : p.N - t.n0 - 1;
+            finite_or_first(acc, a + m * (AT ? 1 : p.lda) + t.k.k0 * (AT ? p.lda : 1), AT ? p.lda : 1,
+                            b + n * (BT ? 1 : p.ldb) + t.k.k0 * (BT ? p.ldb : 1), BT ? p.ldb : 1, t.k.k1 - t.k.k0, lane);
         }
     }
     __syncthreads();

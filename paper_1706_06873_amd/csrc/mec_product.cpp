@@ -56,7 +56,8 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     const bool clean = with.clean;
     const TileCost* const tiles = !dtype ? kF32 : clean ? kBf16 : kBf16Any;
     const int count = dtype && clean ? 5 : 4;
-    const int64_t chunks = ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
+    const int64_t parts = with.two ? 2 : 1;  // chunks of each take turns
+    const int64_t chunks = parts * ceil_div(K, dtype ? 64 : 32), shares = ceil_div(K, 64);
     // A call of one product in shares takes its caller's thread a second launch and a workspace
     // (13 us, so 8; 1 x 2048 x 1000 in bf16 in one launch 7.5 us, in shares 14.0): below that
     // the GPU's time is not what counts. Where other launches stand around it anyway
@@ -73,7 +74,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     };
     const double per_k = !dtype ? 0.0066 : clean ? 0.0027 : layout == Layout::kXKt ? 0.0075 : 0.0040;
     const int64_t small = ceil_div(M, 32) * ceil_div(N, 32) * batch;
-    if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + per_k * (double)K));
+    if (small <= kMaxSmallBlocks) offer(0, 1, (double)ceil_div(small, 256) * (4.0 + per_k * (double)(parts * K)));
     for (int i = 0; i < count; ++i) {
         int64_t n = ceil_div(M, tiles[i].tm) * ceil_div(N, tiles[i].tn);
         if (symmetric && !dtype && i + 1 >= kSymmetricF32) n = (n + ceil_div(M, tiles[i].tm)) / 2;
@@ -83,7 +84,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
             const double ends = tiles[i].ends + (s > 1 ? 0.0 : (with.R ? tiles[i].residual : 0.0) + (with.Z ? tiles[i].saved : 0.0));
-            double us = tile_time(tiles[i], n * real, s > 1 ? per * (dtype ? 1 : 2) : chunks, ends);
+            double us = tile_time(tiles[i], n * real, s > 1 ? parts * per * (dtype ? 1 : 2) : chunks, ends);
             // the sum of the shares: a launch, its reads, and what else moves (the epilogue's
             // output; a mirror image's 4-byte stores)
             if (real > 1) us += (alone ? 4.0 : 3.0) + (double)((alone ? real + 1 : symmetric ? 2 * real : real) * batch * M * N) / 1.2e6;
@@ -94,7 +95,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
 }
 
 ProductPlan plan_pair(const ProductPlan& px, const ProductPlan& pk, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
-                      int32_t max_splits) {
+                      int32_t max_splits, bool two) {
     ProductPlan best{0, 1, 0.0};
     // What two launches take, by their models and a launch's own 3 us; the model of the pair is a
     // little too high (1000 x 1000 x 1000 49 where it took 44, two launches 50; 4608 x 256 x 1024
@@ -105,7 +106,7 @@ ProductPlan plan_pair(const ProductPlan& px, const ProductPlan& pk, int dtype, i
     const int64_t step = dtype ? 64 : 32;
     const int64_t nx = ceil_div(rows, t.tm) * ceil_div(i_c, t.tn), nk = ceil_div(i_c, t.tm) * ceil_div(k_c, t.tn);
     const int64_t shares = ceil_div(rows, 64);
-    auto tile = [&](int64_t chunks) { return (double)chunks * t.chunk[t.fit - 1] + t.ends; };
+    auto tile = [&](int64_t chunks) { return (double)(two ? 2 * chunks : chunks) * t.chunk[t.fit - 1] + t.ends; };
     for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
         if (s > 1 && (shares < 4 * s || s * i_c * k_c > (int64_t(1) << 26))) break;
         const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
@@ -127,7 +128,7 @@ bool clean_rows(Layout layout, const Product& p) {
 }
 
 ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const Product& p) {
-    const Operands with{!dtype || clean_rows(layout, p), p.R != nullptr, p.Z != nullptr};
+    const Operands with{!dtype || clean_rows(layout, p), p.R != nullptr, p.Z != nullptr, p.second != 0};
     return with.clean && !with.R && !with.Z ? plan : plan_product(layout, dtype, p.M, p.N, p.K, 1, plan.splits, false, with);
 }
 

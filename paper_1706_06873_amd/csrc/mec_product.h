@@ -37,6 +37,9 @@ struct Product {
     float diag;      // added to z where m = n
     int32_t symmetric;  // A B and R are symmetric (fp32, no act): the 64 x 64 tiles leave out those above the diagonal
     int32_t y_bf16;  // fp32 products: Y is bf16
+    // bf16, dX and dK: dZ is the sum of two matrices alike, the second (what rounding it to bf16
+    // left over) this many bytes from the first; 0: one matrix
+    int64_t second;
 
     // filled by the launch
     int32_t m_tiles, n_tiles, chunks;  // chunks of the reduction per split
@@ -49,9 +52,10 @@ struct ProductPlan {
     int32_t splits;
     double us;   // by the model
 };
-// What the sizes do not say: 16-byte rows (clean), a residual, a saved argument of the activation.
+// What the sizes do not say: 16-byte rows (clean), a residual, a saved argument of the
+// activation, dZ in two parts.
 struct Operands {
-    bool clean = true, R = false, Z = false;
+    bool clean = true, R = false, Z = false, two = false;
 };
 // max_splits: as many shares as the caller has room for partial sums (batch x M x N each)
 ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t max_splits,
@@ -61,7 +65,7 @@ ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const
 // dX (rows x i_c) and dK (i_c x k_c) by tiles in one launch: kernel 3 and dK's shares, or
 // kernel 0 where two launches by those plans are as fast
 ProductPlan plan_pair(const ProductPlan& x, const ProductPlan& k, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
-                      int32_t max_splits);
+                      int32_t max_splits, bool two);
 // A's and B's rows are whole 16-byte granules (bf16)
 bool clean_rows(Layout layout, const Product& p);
 
@@ -97,11 +101,12 @@ hipError_t launch_sum_parts(const float* part, int64_t count, int64_t n, void* o
 // the same for 2 n columns, the first n to out and the others to out2 (either may be nullptr)
 hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* out, float* out2, hipStream_t stream);
 
-// dZ = G act'(Z) (dZ nullptr: act is none and dZ is G) and, unless nullptr, dbias, by way of
-// the partial column sums of act_grad_shares shares of the rows in part
+// dZ = G act'(Z) (dZ nullptr: act is none and dZ is G) and, unless nullptr, low, what rounding
+// dZ to bf16 left over, rounded to bf16 (both dense), and dbias, by way of the partial column
+// sums of act_grad_shares shares of the rows in part
 int32_t act_grad_shares(int64_t rows, int64_t N);
-hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, float* dbias, float* part, int64_t rows,
-                           int32_t N, int act, int dtype, hipStream_t stream);
+hipError_t launch_act_grad(const void* G, int64_t ldg, const void* Z, void* dZ, void* low, float* dbias, float* part,
+                           int64_t rows, int32_t N, int act, int dtype, hipStream_t stream);
 
 // mec_norm.hip
 hipError_t launch_norm(const void* X, int64_t ldx, const float* gamma, const float* beta, void* Y, int64_t ldy, float* mean,
@@ -498,6 +503,35 @@ __device__ inline void tile_of_half(uint32_t t, uint32_t& mt, uint32_t& nt) {
     while (mt * (mt + 1) / 2 > t) --mt;  // (the root is rounded)
     while ((mt + 1) * (mt + 2) / 2 <= t) ++mt;
     nt = t - mt * (mt + 1) / 2;
+}
+
+// Of dZ's two parts the second is finite, but times an infinity it makes a NaN where it is 0 or of
+// the other sign. Sums that are not finite are therefore taken again from the first part alone,
+// which spreads infinities and NaNs as dZ does; straight from memory: this lane's row of A and
+// column of B, their elements a_k and b_k apart.
+__device__ inline void finite_or_first(floatx16& acc, const uint16_t* a, int64_t a_k, const uint16_t* b, int64_t b_k, int32_t K,
+                                       int lane) {
+    auto odd = [](float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) == 0x7f800000u; };
+    bool any = false;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) any |= odd(acc[v]);
+    if (!__any(any)) return;
+    floatx16 sum = {};
+#pragma clang loop unroll(disable)
+    for (int32_t s = 0; s < K; s += 16) {
+        u32x4v x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t k = s + 8 * (lane >> 5) + e;
+            if (k < K) {
+                x[e / 2] |= (uint32_t)a[k * a_k] << (e % 2 * 16);
+                y[e / 2] |= (uint32_t)b[k * b_k] << (e % 2 * 16);
+            }
+        }
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), __builtin_bit_cast(bf16x8, x), sum, 0, 0, 0);
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = odd(acc[v]) ? sum[v] : acc[v];
 }
 
 // Tile t of a grid of m_tiles x n_tiles: runs of `group` rows of tiles, column by column,

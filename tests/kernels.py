@@ -95,3 +95,35 @@ def product(kernel, layout, A, B, splits=1):
                                   torch.cuda.current_stream().cuda_stream)
     assert r in (0, UNSUPPORTED), (kernel, layout, A.shape, B.shape, r)
     return Y if r == 0 else None
+
+
+class _Operands(ctypes.Structure):  # mec_internal_operands
+    _fields_ = ([(n, _vp) for n in ("A", "B", "Y", "Z", "R", "bias", "part")] +
+                [(n, _i64) for n in ("lda", "ldb", "ldy", "ldz", "ldr", "a_batch", "b_batch", "second")] +
+                [(n, _i) for n in ("splits", "batch", "act", "res_first", "symmetric")] +
+                [(n, ctypes.c_float) for n in ("alpha", "beta", "diag")])
+
+
+_lib.mec_internal_product_with.argtypes = [_i] * 6 + [ctypes.POINTER(_Operands), _vp]
+
+
+def product_with(kernel, layout, A, B, splits=1, R=None, bias=None, act="none", res_first=False, Z=False, alpha=1.0,
+                 beta=1.0, diag=0.0, symmetric=False, second=0, batch=1, Y=None):
+    """product() with an epilogue, in parts (second: bytes to dZ's other part) or for a stack (A
+    and B batch x .., dense): Y, or (Y, Z); None where there is no such kernel."""
+    a, b = (A[0], B[0]) if batch > 1 else (A, B)
+    K, M = a.shape if layout == XTK else a.shape[::-1]
+    N = b.shape[0] if layout == XKT else b.shape[1]
+    stack = (batch,) if batch > 1 else ()
+    if Y is None:
+        Y = torch.full(stack + (M, N), 7.0, dtype=A.dtype, device=A.device)
+    z = torch.full((M, N), 7.0, dtype=A.dtype, device=A.device) if Z else None
+    part = torch.empty(splits * batch * M * N, device=A.device) if splits > 1 else None
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    o = _Operands(ptr(A), ptr(B), ptr(Y), ptr(z), ptr(R), ptr(bias), ptr(part), a.stride(0), b.stride(0), Y.stride(-2), N,
+                  R.stride(-2) if R is not None else 0, A.stride(0) if batch > 1 else 0, B.stride(0) if batch > 1 else 0,
+                  second, splits, batch, mec._ACTS[act], int(res_first), int(symmetric), alpha, beta, diag)
+    r = _lib.mec_internal_product_with(kernel, layout, mec.BF16 if A.dtype == torch.bfloat16 else mec.F32, M, N, K,
+                                       ctypes.byref(o), torch.cuda.current_stream().cuda_stream)
+    assert r in (0, UNSUPPORTED), (kernel, layout, A.shape, B.shape, r)
+    return None if r else (Y, z) if Z else Y

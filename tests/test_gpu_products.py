@@ -1,0 +1,169 @@
+"""The products of the layer operators, kernel by kernel, and what their sums are made of, on
+the GPU against 64 bits on the CPU.
+
+Bounds are by arithmetic: n products added in fp32, cut off rather than rounded at worst, are off
+by at most n 2^-23 times the sum of the products' magnitudes, in any order; rounding to bf16 is
+monotonic, so a bf16 output lies between the roundings of the two ends of its interval."""
+import math
+
+import pytest
+import torch
+
+import kernels as kn
+import paper_1706_06873_amd as mec
+from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, close, randn, rows_of, slope64
+
+pytestmark = pytest.mark.gpu
+
+
+def within(got, want, err, what, decided=0.0):
+    """got (bf16) is a rounding of a value within err of want; for `decided` of the elements at
+    least there is only one such (that many the test can decide on: err grows as the number n of
+    products, the outputs as its root, so about n^1.5 2^-14 of them it cannot)."""
+    lo, hi = (want - err).to(BF16), (want + err).to(BF16)
+    got = got.detach().cpu().reshape(want.shape)
+    assert (got >= lo).all() and (got <= hi).all(), (what, int(((got < lo) | (got > hi)).sum()), want.numel())
+    share = float((lo == hi).double().mean())
+    assert share >= decided, (what, share)
+
+
+def slope_without_cancellation(act, z):
+    """act'(z) in 64 bits by s(t) and 1 - s(t) = s(-t), for what the sign of a small slope decides: at
+    z = -7.25 the GELU's is -1.35e-15 (s = 1.9e-16, times 1 + z 2u' (1 - s)), where 1 + tanh is 0."""
+    t = z if act == "silu" else 2 * C0 * (z + 0.044715 * z ** 3)
+    s, q = torch.sigmoid(t), torch.sigmoid(-t)
+    return s + z * s * q * (1 if act == "silu" else 2 * C0 * (1 + 0.134145 * z * z))
+
+
+# ---------------------------------------------------------------- dZ with more bits than bf16
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,i_c,k_c", [(40, 72, 48), (150, 200, 136), (61, 131, 77), (5, 100, 33), (300, 256, 40),
+                                          (128, 1024, 1024), (200, 1001, 1024), (64, 4096, 128)])
+def test_gradients_in_bf16_take_dz_before_its_rounding(rows, i_c, k_c, act):
+    """dX and dK are the correctly rounded products of dZ to 16 bits, element by element, wherever
+    the bound leaves one rounding; products of dZ as rounded to bf16 miss about every third."""
+    g = torch.Generator().manual_seed(rows + i_c)
+    X, K = randn(g, rows, i_c).to(BF16), (randn(g, i_c, k_c) / math.sqrt(i_c)).to(BF16)
+    G, Z = randn(g, rows, k_c).to(BF16), (2 * randn(g, rows, k_c)).to(BF16)
+    print("[case]", rows, i_c, k_c, act, flush=True)
+    dX, dK, _, dZ = mec.linear_grad(G.to(DEV), X.to(DEV), K.to(DEV), Z.to(DEV), act)
+    x, k, q = X.double(), K.double(), G.double()
+    dz = q * slope64(act, Z.double())
+    # the slope's evaluation, and what is left over of two roundings to bf16
+    ez = q.abs() * 2.0 ** -15 + dz.abs() * 2.0 ** -16
+    close(dZ, dz, q.abs() * 2.0 ** -15 + HALF[BF16] * (dz.abs() + q.abs() * 2.0 ** -15), "dZ")
+    ex = (2 * k_c + 8) * 2.0 ** -23 * (dz.abs() @ k.abs().T) + 1.01 * (ez @ k.abs().T)
+    within(dX, dz @ k.T, ex, "dX", 0.5 if k_c <= 300 else 0.0)
+    ek = (2 * rows + 8) * 2.0 ** -23 * (x.abs().T @ dz.abs()) + 1.01 * (x.abs().T @ ez)
+    within(dK, x.T @ dz, ek, "dK", 0.5 if rows <= 150 else 0.0)
+
+
+PARTS = [(300, 280, 200, 0, 1), (257, 264, 64, 8, 1), (130, 67, 77, 3, 1), (5, 9, 300, 0, 1), (264, 520, 328, 0, 1),
+         (72, 40, 1024, 0, 3), (33, 200, 517, 5, 2), (520, 264, 96, 0, 1)]
+
+
+def two_parts(dz, gap, order):
+    """dZ's two parts in one allocation, the first after the second where order is -1, and the
+    bytes from the one to the other."""
+    first = dz.to(BF16)
+    second = (dz - first.double()).to(BF16)
+    both = torch.full((2, dz.shape[0] + 1, dz.shape[1] + gap), 7.0, dtype=BF16, device=DEV)
+    at = (0, 1) if order > 0 else (1, 0)
+    for i, t in zip(at, (first, second)):
+        both[i, :dz.shape[0], :dz.shape[1]] = t.to(DEV)
+    view = both[at[0], :dz.shape[0], :dz.shape[1]]
+    return view, order * both.stride(0) * 2, first.double() + second.double()
+
+
+@pytest.mark.parametrize("layout", [kn.XKT, kn.XTK])
+def test_every_kernel_on_dz_in_two_parts(layout):
+    ran = 0
+    for M, N, K, gap, splits in PARTS:
+        g = torch.Generator().manual_seed(M + N + K)
+        order = 1 if K % 2 else -1
+        if layout == kn.XKT:  # dZ is A
+            dz, b = randn(g, M, K).double(), randn(g, K, N).to(BF16)
+            A, second, a = two_parts(dz, gap, order)
+            b, B = b.double(), rows_of(b.T.contiguous(), gap)
+        else:
+            a, dz = randn(g, M, K).to(BF16), randn(g, K, N).double()
+            B, second, b = two_parts(dz, gap, order)
+            a, A = a.double(), rows_of(a.T.contiguous(), gap)
+        err = (2 * K + 8) * 2.0 ** -23 * 1.01 * (a.abs() @ b.abs())
+        for kernel in range(6):
+            if splits > 1 and kernel == 0:
+                continue
+            print("[case]", layout, M, N, K, gap, splits, kernel, flush=True)
+            Y = kn.product_with(kernel, layout, A, B, splits, second=second)
+            within(Y, a @ b, err, kernel, 0.5 if K < 300 else 0.0)
+            ran += 1
+    assert ran >= 40
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,i_c,k_c", [(40, 72, 48), (150, 201, 136), (2000, 296, 304), (600, 1100, 1000)])
+def test_gradients_in_bf16_spread_infinities_and_nans(rows, i_c, k_c, act):
+    """As the formulas do from dZ, whatever its second part: infinities in K and X times dZ of either
+    sign, and infinities and NaNs in G."""
+    g = torch.Generator().manual_seed(17)
+    X, K, G = randn(g, rows, i_c), randn(g, i_c, k_c), randn(g, rows, k_c)
+    Z = 2 * randn(g, rows, k_c)
+    K[3, 5], K[7, k_c - 1], X[4, 2], X[rows - 1, i_c - 1] = math.inf, -math.inf, -math.inf, math.inf
+    G[9, 1], G[11, 30], X[20, 8] = math.inf, math.nan, math.nan
+    G[13, 5] = 0.0  # a dZ of 0 times an infinity
+    X, K, G, Z = (t.to(BF16) for t in (X, K, G, Z))
+    print("[case]", rows, i_c, k_c, act, flush=True)
+    dX, dK, _, dZ = (t.cpu() for t in mec.linear_grad(G.to(DEV), X.to(DEV), K.to(DEV), Z.to(DEV), act))
+    dz = G.double() * slope_without_cancellation(act, Z.double())
+    assert torch.equal(torch.isnan(dZ), torch.isnan(dz)) and torch.equal(torch.isinf(dZ), torch.isinf(dz))
+    for got, want in ((dX, dz @ K.double().T), (dK, X.double().T @ dz)):
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isposinf(got), torch.isposinf(want))
+        assert torch.equal(torch.isneginf(got), torch.isneginf(want))
+        ok = torch.isfinite(want)
+        # (finite sums of up to 2000 products of order 1: bf16's half step, and far more than the sums' own error)
+        assert ((got.double() - want).abs()[ok] <= HALF[BF16] * want.abs()[ok] + 2.0 ** -6).all()
+
+
+def test_gradients_in_bf16_do_not_touch_what_lies_behind_the_workspace():
+    """The workspace of exactly the size asked for, at every 4-byte alignment."""
+    g = torch.Generator().manual_seed(18)
+    for rows, i_c, k_c in ((70, 24, 40), (2000, 33, 57), (700, 512, 64)):
+        X, K, G, Z = (randn(g, *s).to(BF16).to(DEV) for s in ((rows, i_c), (i_c, k_c), (rows, k_c), (rows, k_c)))
+        want = mec.linear_grad(G, X, K, Z, "gelu")
+        need = mec.linear_grad_workspace_bytes(rows, i_c, k_c, mec.BF16, "gelu")
+        for shift in (0, 4, 8, 12):
+            ws = torch.full((need + 80,), 0x7f, dtype=torch.uint8, device=DEV)
+            print("[case]", rows, i_c, k_c, shift, flush=True)
+            got = mec.linear_grad(G, X, K, Z, "gelu", workspace=ws[shift:shift + need + (-need) % 4][:need])
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            assert (ws[:shift] == 0x7f).all() and (ws[shift + need:] == 0x7f).all()
+
+
+def test_gradients_in_bf16_captured_and_in_place():
+    """dZ in the memory of Z and of G, and a graph replayed between eager calls of the same."""
+    g = torch.Generator().manual_seed(19)
+    inputs = [[randn(g, *s).to(BF16).to(DEV) for s in ((300, 72), (72, 136), (300, 136), (300, 136))] for _ in range(3)]
+    X, K, G, Z = inputs[0]
+    want = mec.linear_grad(G, X, K, Z, "silu")
+    z, q = Z.clone(), G.clone()
+    got = mec.linear_grad(G, X, K, z, "silu", dZ=z)
+    assert got[3] is z and all(torch.equal(a, b) for a, b in zip(got, want))
+    got = mec.linear_grad(q, X, K, Z, "silu", dZ=q)
+    assert got[3] is q and all(torch.equal(a, b) for a, b in zip(got, want))
+    fixed = [t.clone() for t in inputs[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        mec.linear_grad(fixed[2], fixed[0], fixed[1], fixed[3], "gelu")
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = mec.linear_grad(fixed[2], fixed[0], fixed[1], fixed[3], "gelu")
+    for given in inputs[::-1]:
+        want = mec.linear_grad(given[2], given[0], given[1], given[3], "gelu")
+        for t, v in zip(fixed, given):
+            t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
