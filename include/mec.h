@@ -314,7 +314,8 @@ int mec_conv2d_wgrad_noalloc(const void* I, const float* G, float* dK,
  * `dtype` is the type of the activations, their gradients, K and dK; bias,
  * gamma, beta, their gradients and the row statistics are fp32, and so is
  * everything between: each output is rounded once. Widths and pitches go up to
- * 2^20, rows to 2^30 (MEC_ERR_UNSUPPORTED beyond). Results are reproducible:
+ * 2^20, rows to 2^30 (MEC_ERR_UNSUPPORTED beyond, and for outputs of terabytes, more tiles
+ * than a launch holds). Results are reproducible:
  * every sum has an order fixed by the sizes, the alignments, the activation and which
  * operands are given (no atomics).
  * Infinities and NaNs spread as in the formulas.

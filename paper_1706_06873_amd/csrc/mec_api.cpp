@@ -419,16 +419,18 @@ int mec_linear(const void* X, const void* K, const float* bias, const void* R, v
     p.alpha = p.beta = 1.0f;
     p.batch = 1;
     p.part = static_cast<float*>(workspace);
+    const mec::ProductPlan refined = mec::refine_plan(plan, mec::Layout::kXK, dtype, p);
+    if (refined.kernel < 0) return MEC_ERR_UNSUPPORTED;
     clear_stale_error();
-    return hip_status(launch_shared(mec::refine_plan(plan, mec::Layout::kXK, dtype, p), mec::Layout::kXK, p, dtype,
-                                    (hipStream_t)stream), "linear");
+    return hip_status(launch_shared(refined, mec::Layout::kXK, p, dtype, (hipStream_t)stream), "linear");
 }
 
 int64_t mec_linear_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
     const int rc = first_error({check_rows(rows, i_c, i_c), check_rows(rows, k_c, k_c)});
     if (rc != MEC_OK) return rc;
     if (!valid_dtype(dtype)) return MEC_ERR_INVALID_ARG;
-    return parts_bytes(linear_plan(rows, i_c, k_c, dtype), rows, k_c);
+    const mec::ProductPlan plan = linear_plan(rows, i_c, k_c, dtype);
+    return plan.kernel < 0 ? MEC_ERR_UNSUPPORTED : parts_bytes(plan, rows, k_c);
 }
 
 int64_t mec_linear_grad_workspace_bytes(int64_t rows, int i_c, int k_c, int dtype) {
@@ -460,6 +462,7 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     if ((dX || dK || dbias) && plan.bytes && (!workspace || (uint64_t)workspace_bytes < (uint64_t)plan.bytes))
         return MEC_ERR_WORKSPACE;
     if (!aligned(workspace, 4)) return MEC_ERR_ALIGNMENT;
+    if ((dX && plan.x.kernel < 0) || (dK && plan.k.kernel < 0)) return MEC_ERR_UNSUPPORTED;  // (the same with other operands)
     const hipStream_t st = (hipStream_t)stream;
     float* const part = static_cast<float*>(workspace);
     char* const low = plan.two && (dX || dK) ? reinterpret_cast<char*>(((uintptr_t)workspace + plan.sums + 15) / 16 * 16) : nullptr;
@@ -688,7 +691,7 @@ int mec_internal_product_with(int kernel, int layout, int dtype, int M, int N, i
 
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
     const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? kMaxShares : 1);
-    return p.kernel + 16 * p.splits;
+    return p.kernel < 0 ? MEC_ERR_UNSUPPORTED : p.kernel + 16 * p.splits;
 }
 
 int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits, int M, int N,

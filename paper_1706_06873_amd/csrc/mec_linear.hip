@@ -372,7 +372,7 @@ uint32_t prepare(Product& p) {
     const int64_t chunks = 64 / KT * (((int64_t)p.K + 63) / 64);
     p.chunks = 64 / KT * (int32_t)((chunks / (64 / KT) + p.splits - 1) / p.splits);
     const int64_t blocks = (int64_t)p.m_tiles * p.n_tiles * p.splits;
-    return blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
+    return blocks > kMaxThreads / C::THREADS || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
 }
 
 template <int BM, int BN, int WM, int WN, int KT, int S, Layout L>
@@ -408,7 +408,7 @@ hipError_t launch_product_bf16_pair(Product x, Product k, hipStream_t stream) {
     using K = Cfg<1, 2, 2, 2, 64, 2, Layout::kXtK, true>;
     if (!clean_rows(Layout::kXKt, x) || !clean_rows(Layout::kXtK, k)) return hipErrorInvalidValue;
     const uint32_t bx = prepare<X>(x), bk = prepare<K>(k);
-    if (!bx || !bk || bx > 0x7fffffffu - bk) return hipErrorInvalidValue;
+    if (!bx || !bk || (int64_t)bx + bk > kMaxThreads / X::THREADS) return hipErrorInvalidValue;
     hipLaunchKernelGGL((product_bf16_pair_kernel<X, K>), dim3(bx + bk), dim3(X::THREADS), 0, stream, x, k, bx);
     return hipGetLastError();
 }

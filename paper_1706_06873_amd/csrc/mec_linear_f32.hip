@@ -304,7 +304,7 @@ uint32_t prepare(Product& p) {
     p.chunks = 2 * (int32_t)((chunks / 2 + p.splits - 1) / p.splits);
     const int64_t tiles = p.symmetric ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles;
     const int64_t blocks = tiles * p.splits * p.batch;
-    return blocks > 0x7fffffff || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
+    return blocks > kMaxThreads / (C::THREADS * C::kKW) || (p.splits - 1) * (int64_t)p.chunks >= chunks ? 0 : (uint32_t)blocks;
 }
 
 template <int BM, int BN, int WM, int WN, int KW, Layout L>
@@ -341,7 +341,7 @@ hipError_t launch_product_f32_pair(Product x, Product k, hipStream_t stream) {
     using XTail = Cfg<1, 1, 2, 2, 1, Layout::kXKt, true>;
     using K = Cfg<1, 1, 2, 2, 1, Layout::kXtK, false>;
     const uint32_t bx = prepare<X>(x), bk = prepare<K>(k);
-    if (!bx || !bk || bx > 0x7fffffffu - bk) return hipErrorInvalidValue;
+    if (!bx || !bk || (int64_t)bx + bk > kMaxThreads / X::THREADS) return hipErrorInvalidValue;
     const dim3 grid(bx + bk), block(X::THREADS);
     if (x.K % 8) hipLaunchKernelGGL((product_f32_pair_kernel<XTail, K>), grid, block, 0, stream, x, k, bx);
     else hipLaunchKernelGGL((product_f32_pair_kernel<X, K>), grid, block, 0, stream, x, k, bx);

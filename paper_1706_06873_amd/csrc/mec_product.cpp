@@ -14,28 +14,28 @@ namespace mec {
 namespace {
 
 struct TileCost {
-    int tm, tn, fit;
+    int tm, tn, threads, fit;
     double chunk[5], ends, residual, saved;  // residual, saved: what R and Z add to the ends
 };
 // by the kernels' numbers, from 1. Large tiles wait longer for a residual than small ones, of
 // which others run meanwhile: 1577088 x 64 -> 256 in bf16 281, 239, 297, 367 us, with Z 440, 409,
 // 458, 555, with R 415, 367, 329, 365, with both 531, 496, 455, 499; in fp32 744, 661, 804, with Z
 // 1128, 1000, 1219, with R 833, 819, 970, with both 1031, 1087, 1178.
-constexpr TileCost kBf16[] = {{128, 128, 2, {0.57, 1.00}, 4.2, 2.5, 3.6},
-                              {256, 256, 1, {1.45}, 8.5, 5.3, 6.8},
-                              {64, 128, 3, {0.40, 0.70, 0.85}, 3.5, 0.4, 2.2},
-                              {64, 64, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4, 0.0, 2.2},
-                              {64, 64, 2, {0.26, 0.38}, 3.8, 0.4, 1.0}};
+constexpr TileCost kBf16[] = {{128, 128, 256, 2, {0.57, 1.00}, 4.2, 2.5, 3.6},
+                              {256, 256, 512, 1, {1.45}, 8.5, 5.3, 6.8},
+                              {64, 128, 256, 3, {0.40, 0.70, 0.85}, 3.5, 0.4, 2.2},
+                              {64, 64, 256, 5, {0.32, 0.50, 0.65, 0.80, 0.85}, 3.4, 0.0, 2.2},
+                              {64, 64, 256, 2, {0.26, 0.38}, 3.8, 0.4, 1.0}};
 // the same by way of registers (rows that are no whole 16-byte granules): 1886 x 3185 -> 2368
 // 95, 157, 81, 110 where 3184 takes 50, 62, 50, 62; 11471 x 2505 -> 48 65, 124, 51, 43
-constexpr TileCost kBf16Any[] = {{128, 128, 2, {1.50, 1.80}, 4.2, 2.5, 3.6},
-                                 {256, 256, 1, {2.90}, 8.5, 5.3, 6.8},
-                                 {64, 128, 3, {1.19, 1.35, 1.55}, 3.5, 0.4, 2.2},
-                                 {64, 64, 5, {0.80, 1.10, 1.45, 1.80, 2.10}, 3.4, 0.0, 2.2}};
-constexpr TileCost kF32[] = {{128, 64, 2, {0.90, 1.55}, 4.8, 0.9, 3.2},
-                             {256, 128, 1, {2.3}, 10.0, 3.3, 6.5},
-                             {64, 64, 3, {0.64, 0.95, 1.15}, 5.0, 1.0, 2.5},
-                             {64, 64, 1, {0.48}, 7.0, 1.0, 2.5}};
+constexpr TileCost kBf16Any[] = {{128, 128, 256, 2, {1.50, 1.80}, 4.2, 2.5, 3.6},
+                                 {256, 256, 512, 1, {2.90}, 8.5, 5.3, 6.8},
+                                 {64, 128, 256, 3, {1.19, 1.35, 1.55}, 3.5, 0.4, 2.2},
+                                 {64, 64, 256, 5, {0.80, 1.10, 1.45, 1.80, 2.10}, 3.4, 0.0, 2.2}};
+constexpr TileCost kF32[] = {{128, 64, 256, 2, {0.90, 1.55}, 4.8, 0.9, 3.2},
+                             {256, 128, 512, 1, {2.3}, 10.0, 3.3, 6.5},
+                             {64, 64, 256, 3, {0.64, 0.95, 1.15}, 5.0, 1.0, 2.5},
+                             {64, 64, 768, 1, {0.48}, 7.0, 1.0, 2.5}};
 
 constexpr int kPair = 3;          // the kernel whose tiles a pair of products takes
 constexpr int kSymmetricF32 = 3;  // the fp32 kernels from this one on have square tiles
@@ -63,7 +63,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
     // the GPU's time is not what counts. Where other launches stand around it anyway
     // (dK, a symmetric product) it is.
     const bool alone = layout != Layout::kXtK && !symmetric;
-    ProductPlan best{0, 1, 1e30};
+    ProductPlan best{-1, 1, 1e30};
     double least = 1e30;
     auto offer = [&](int32_t kernel, int64_t splits, double us) {
         const double host = !alone ? 0.0 : splits > 1 ? 13.0 : 8.0, t = us > host ? us : host;
@@ -83,6 +83,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
             // shares of at least 4 chunks of 64, none empty, and partial sums of at most 256 MB
             if (s > 1 && (shares < 4 * s || s * batch * M * N > (int64_t(1) << 26))) break;
             const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
+            if (n * real > kMaxThreads / tiles[i].threads) break;
             const double ends = tiles[i].ends + (s > 1 ? 0.0 : (with.R ? tiles[i].residual : 0.0) + (with.Z ? tiles[i].saved : 0.0));
             double us = tile_time(tiles[i], n * real, s > 1 ? parts * per * (dtype ? 1 : 2) : chunks, ends);
             // the sum of the shares: a launch, its reads, and what else moves (the epilogue's
@@ -110,6 +111,7 @@ ProductPlan plan_pair(const ProductPlan& px, const ProductPlan& pk, int dtype, i
     for (int64_t s = 1; s <= max_splits; s = s < 4 ? s + 1 : s + s / 4) {
         if (s > 1 && (shares < 4 * s || s * i_c * k_c > (int64_t(1) << 26))) break;
         const int64_t per = ceil_div(shares, s), real = ceil_div(shares, per);
+        if (nx + nk * real > kMaxThreads / t.threads) break;
         const double x = tile(ceil_div(k_c, step)), k = tile(real > 1 ? per * 64 / step : ceil_div(rows, step));
         // the compute units are full but for the last tile's time
         double us = ((double)nx * x + (double)(nk * real) * k) / (256.0 * t.fit);
@@ -135,6 +137,7 @@ ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream) {
     p.splits = plan.splits;
     p.symmetric = p.symmetric && !dtype && plan.kernel >= kSymmetricF32;
+    if (plan.kernel < 0) return hipErrorNotSupported;
     if (plan.kernel == 0) return p.splits > 1 ? hipErrorNotSupported : launch_product_small(layout, p, dtype, stream);
     return dtype ? launch_product_bf16(layout, p, plan.kernel, stream) : launch_product_f32(layout, p, plan.kernel, stream);
 }

@@ -46,9 +46,12 @@ struct Product {
     int32_t clean;                     // 16-byte rows of A and B
 };
 
+// What a launch holds in one dimension of its grid.
+constexpr int64_t kMaxThreads = (int64_t(1) << 32) - 1;
+
 // Which kernel computes a product, and the shares of its reduction.
 struct ProductPlan {
-    int kernel;  // 0 the small one, from 1 the tiles
+    int kernel;  // 0 the small one, from 1 the tiles; -1: more outputs than a launch of any holds
     int32_t splits;
     double us;   // by the model
 };
@@ -63,7 +66,7 @@ ProductPlan plan_product(Layout layout, int dtype, int64_t M, int64_t N, int64_t
 // the plan by the sizes alone, for the operands as they are: in no more shares
 ProductPlan refine_plan(const ProductPlan& plan, Layout layout, int dtype, const Product& p);
 // dX (rows x i_c) and dK (i_c x k_c) by tiles in one launch: kernel 3 and dK's shares, or
-// kernel 0 where two launches by those plans are as fast
+// kernel 0 where two launches by those plans are as fast, or one does not hold both
 ProductPlan plan_pair(const ProductPlan& x, const ProductPlan& k, int dtype, int64_t rows, int64_t i_c, int64_t k_c,
                       int32_t max_splits, bool two);
 // A's and B's rows are whole 16-byte granules (bf16)

@@ -167,3 +167,23 @@ def test_gradients_in_bf16_captured_and_in_place():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+# ---------------------------------------------------------------- as many rows as a call may have
+
+def test_as_many_rows_as_there_may_be():
+    """2^30 rows of one channel: more tiles of 64 rows than a launch holds. One product per output,
+    so the exact one rounded."""
+    rows = 1 << 30
+    X = torch.empty(rows, 1, dtype=BF16, device=DEV)
+    X[:, 0] = torch.arange(rows, device=DEV, dtype=torch.int32).remainder_(997).to(BF16)
+    K = torch.tensor([[1.2421875]], dtype=BF16, device=DEV)
+    print("[case] linear", flush=True)
+    Y = mec.linear(X, K)
+    for i in range(0, rows, rows // 4):
+        assert torch.equal(Y[i:i + rows // 4], X[i:i + rows // 4] * K)
+    del Y
+    print("[case] dX", flush=True)
+    dX = mec.linear_grad(X, None, K, needs=(True, False, False))[0]
+    for i in range(0, rows, rows // 4):
+        assert torch.equal(dX[i:i + rows // 4], X[i:i + rows // 4] * K)

@@ -7,7 +7,7 @@ import torch
 
 import kernels as kn
 import paper_1706_06873_amd as mec
-from test_layers import BF16, F32, FAKE, NULL, linear_grad
+from test_layers import BF16, F32, NULL, linear, linear_grad
 
 
 def test_workspaces_by_activation():
@@ -40,3 +40,31 @@ def test_the_binding_asks_for_the_workspace_of_its_activation():
     for act in ("none", "relu"):
         with pytest.raises(ValueError, match="device tensor"):
             mec.linear_grad(G, X, K, Z, act, workspace=small)
+
+
+# outputs and threads of a workgroup, by the kernels' numbers
+TILES = {"f32": {0: (32, 32, 1024), 1: (128, 64, 256), 2: (256, 128, 512), 3: (64, 64, 256), 4: (64, 64, 768)},
+         "bf16": {0: (32, 32, 1024), 1: (128, 128, 256), 2: (256, 256, 512), 3: (64, 128, 256), 4: (64, 64, 256),
+                  5: (64, 64, 256)}}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", [kn.XK, kn.XKT])
+@pytest.mark.parametrize("rows,width", [(1 << 30, 1), (1 << 30, 16), (1 << 30, 64), ((1 << 30) - 63, 8), (1 << 29, 128),
+                                        (1 << 28, 256), (1 << 25, 2048), (1 << 24, 64)])
+def test_plans_are_launches_that_a_grid_holds(dtype, layout, rows, width):
+    """Fewer than 2^32 threads, for products of many rows as for a stack of many matrices."""
+    for K in (1, 16, 64, 1024):
+        for M, batch in ((rows, 1), (rows >> 14, 1 << 14)):
+            kernel, shares = kn.product_plan(layout, dtype, M, width, K, batch, batch == 1)
+            tm, tn, threads = TILES[dtype][kernel]
+            blocks = -(-M // tm) * -(-width // tn) * batch * shares
+            assert blocks * threads < 1 << 32, (kernel, shares, K, batch)
+
+
+def test_outputs_that_no_launch_holds_are_refused():
+    """2^40 of them, terabytes: nothing is launched, and nothing before it either."""
+    big = dict(rows=1 << 30, k_c=1024, xp=5, rp=1024, yp=1024)
+    assert linear(**big) == -5 and linear(dtype=BF16, **big) == -5
+    assert mec.lib.mec_linear_workspace_bytes(1 << 30, 5, 1024, F32) == -5
+    assert linear_grad(rows=1 << 30, i_c=1024, k_c=5, gp=5, xp=1024, wb=1 << 62) == -5
