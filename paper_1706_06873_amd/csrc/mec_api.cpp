@@ -689,6 +689,10 @@ int mec_internal_product_with(int kernel, int layout, int dtype, int M, int N, i
     return hip_status(mec::launch_sum_parts(o->part, o->splits, (int64_t)o->batch * M * N, o->Y, dtype, st), "sum");
 }
 
+int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, float b, float c) {
+    return mec::orth_pairs(batch, rows, cols, steps, a, b, c);
+}
+
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
     const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? kMaxShares : 1);
     return p.kernel < 0 ? MEC_ERR_UNSUPPORTED : p.kernel + 16 * p.splits;

@@ -236,6 +236,8 @@ extern "C" int mec_internal_dgrad_gemm(int tile, const float* G, const float* K,
                                        int i_c, int k_h, int k_w, int k_c, int s_h, int s_w, void* stream);
 // The kernel that a product of the layer operators takes, plus 16 times its shares.
 extern "C" int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split);
+// Whether an orthogonalisation takes its first and its last two steps as one.
+extern "C" int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, float b, float c);
 // A plain product of the layer operators (mec_product.h) by one kernel: 0 the small one, from
 // 1 the tile kernels; Y's rows are dense where splits > 1 (part: splits x M x N floats).
 extern "C" int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits,

@@ -9,13 +9,19 @@
 // pair of steps needs one Gram matrix of X and one product with X, for P' P, and the rest on
 // m x m matrices (which commute, being polynomials of A): P A, (P A) P and P' P. In products
 // of m x m x m that is 2r + 5 against 4r + 2. The error of A is relative to its largest value,
-// and a step multiplies it in the small singular directions, so a pair costs nothing where
+// and a step multiplies it in the small singular directions, so a pair costs least where
 // all singular values are alike or what it spoils is not multiplied again: the first two
 // steps (all below the polynomial's range yet) and the last two. The steps between them are
-// taken one by one. With 5 steps, 2 + 1 + 2 stay within 1.7 of the single steps' error
-// against 64 bits (1.1 at the median; 4e-7 to 4e-5 over Gaussian, low-rank, log-spaced and
-// two-valued spectra of 16 x 64 to 200 x 400); 1 + 2 + 2 lose up to 6 times, 3 + 2 up to 12
-// (thin matrices), 5 at once up to 70.
+// taken one by one. What a pair loses depends on the steps around it and on the coefficients:
+// error against 64 bits over that of single steps, worst of Gaussian, low-rank, two-valued and
+// log-spaced spectra of 256 x 2304, 53 x 2016, 32 x 2160, 200 x 400 and 128 x 1152,
+//   3.4445, -4.7750, 2.0315   5 to 10 steps 1.7 (1.0 to 1.1 at the median), but 2 steps 3.8, 4 (as
+//                             2 + 2) 3.2, and 5 as 1 + 2 + 2 6, as 3 + 2 12, at once 70
+//   1.5, -0.5, 0              2 steps 6.4, 5 steps 6.1
+//   1.875, -1.25, 0.375       2 steps 3.4
+//   2, -1.5, 0.5              4 steps 3.6, 5 steps 2.5
+//   4, -6, 2.5                3 steps 3.1, 5 steps 19
+// so that only 5 steps and more with the first of these are taken so; all others singly.
 #include "mec_product.h"
 
 namespace mec {
@@ -121,8 +127,12 @@ int32_t gram_shares(int64_t m, int32_t batch) {
     return (int32_t)(fit < 6 ? 6 : fit < 32 ? fit : 32);
 }
 
-// A pair of steps at once: the modelled times of the products that differ.
-bool pairs_preferred(int64_t m, int64_t n, int32_t batch) {
+// A pair of steps at once loses less than twice a single step's precision (above) ...
+bool pairs_precise(int32_t steps, float a, float b, float c) {
+    return steps >= 5 && a == 3.4445f && b == -4.7750f && c == 2.0315f;
+}
+// ... and is faster: the modelled times of the products that differ.
+bool pairs_faster(int64_t m, int64_t n, int32_t batch) {
     auto us = [&](int64_t M, int64_t N, int64_t K) { return plan_product(Layout::kXKt, 0, M, N, K, batch, 1, M == N).us; };
     return us(m, m, n) + us(n, m, m) > 3 * us(m, m, m);
 }
@@ -135,7 +145,19 @@ bool step_preferred(int64_t m, int64_t rows, int64_t cols, int32_t batch) {
     return m <= kOrthStepMax && rows <= 2048 && cols <= 2048 && ((rows + 31) / 32) * ((cols + 31) / 32) * batch <= 256;
 }
 
+// How the steps are taken: by products, in a launch each, or in pairs at both ends.
+enum class Steps { kSingle, kOneLaunch, kPairs };
+Steps plan_steps(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float a, float b, float c) {
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (step_preferred(m, rows, cols, batch)) return Steps::kOneLaunch;
+    return pairs_precise(steps, a, b, c) && pairs_faster(m, n, batch) ? Steps::kPairs : Steps::kSingle;
+}
+
 }  // namespace
+
+bool orth_pairs(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float a, float b, float c) {
+    return plan_steps(batch, rows, cols, steps, a, b, c) == Steps::kPairs;
+}
 
 // Two copies of X, the m x m matrices and the partial norms; the output is the second copy's
 // last use.
@@ -192,7 +214,8 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         e = launch_product(Layout::kXKt, p, 0, stream);
     };
     int copy = 0;
-    const bool one = step_preferred(m, rows, cols, batch), pairs = !one && pairs_preferred(m, n, batch);
+    const Steps how = plan_steps(batch, rows, cols, steps, a, b, c);
+    const bool one = how == Steps::kOneLaunch, pairs = how == Steps::kPairs;
     for (int32_t left = steps; left > 0 && e == hipSuccess;) {
         const bool two = pairs && left >= 2 && (left == steps || left == 2);
         left -= two ? 2 : 1;

@@ -127,3 +127,11 @@ def product_with(kernel, layout, A, B, splits=1, R=None, bias=None, act="none", 
                                        ctypes.byref(o), torch.cuda.current_stream().cuda_stream)
     assert r in (0, UNSUPPORTED), (kernel, layout, A.shape, B.shape, r)
     return None if r else (Y, z) if Z else Y
+
+
+_lib.mec_internal_orth_pairs.argtypes = [_i] * 4 + [ctypes.c_float] * 3
+
+
+def orth_pairs(batch, rows, cols, steps=5, coefficients=(3.4445, -4.7750, 2.0315)):
+    """Whether an orthogonalisation takes its first and its last two steps as one."""
+    return bool(_lib.mec_internal_orth_pairs(batch, rows, cols, steps, *coefficients))

@@ -11,7 +11,7 @@ import torch
 
 import kernels as kn
 import paper_1706_06873_amd as mec
-from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, close, randn, rows_of, slope64
+from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, close, orth64, randn, rows_of, slope64
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +187,33 @@ def test_as_many_rows_as_there_may_be():
     dX = mec.linear_grad(X, None, K, needs=(True, False, False))[0]
     for i in range(0, rows, rows // 4):
         assert torch.equal(dX[i:i + rows // 4], X[i:i + rows // 4] * K)
+
+
+# ---------------------------------------------------------------- orthogonalisation
+
+DEFAULT = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 256, 2304), (6, 2016, 53), (2, 32, 2160), (4, 200, 400), (3, 128, 1152)])
+@pytest.mark.parametrize("noise", [1.0, 0.3])
+def test_any_steps_and_coefficients_are_as_precise_as_plain_steps(batch, rows, cols, noise):
+    """At most twice the error of the same steps taken one by one in fp32, whose roundings are as many
+    and whose sums are ordered otherwise, and one rounding, 2^-24, for what products in six parts
+    leave out. (The norm of the plain steps is taken in 64 bits, as the kernels' is.)"""
+    g = torch.Generator().manual_seed(rows + 1)
+    k = max(1, min(rows, cols) // 8)
+    U = randn(g, batch, rows, k) @ randn(g, batch, k, cols) / k ** 0.5 * (noise < 1) + noise * randn(g, batch, rows, cols)
+    X0 = U.mT.contiguous() if rows > cols else U
+    for co, steps in ((DEFAULT, 1), (DEFAULT, 2), (DEFAULT, 3), (DEFAULT, 4), (DEFAULT, 5), (DEFAULT, 6), ((1.5, -0.5, 0.0), 2),
+                      ((1.5, -0.5, 0.0), 5), ((1.875, -1.25, 0.375), 2), ((2.0, -1.5, 0.5), 4), ((2.0, -1.5, 0.5), 5)):
+        a, b, c = co
+        X = (X0.double() / (X0.double().flatten(1).norm(dim=1).view(-1, 1, 1) + 1e-7)).float()
+        for _ in range(steps):
+            A = X @ X.mT.contiguous()
+            X = a * X + (b * A + c * (A @ A)) @ X
+        plain = X.mT if rows > cols else X
+        want = orth64(U, steps, co)
+        print("[case]", batch, rows, cols, noise, co, steps, flush=True)
+        got = mec.orthogonalize(U.to(DEV), steps=steps, coefficients=co).cpu()
+        err = lambda x: ((x.double() - want).norm() / want.norm()).item()  # noqa: E731
+        assert err(got) <= 2 * err(plain) + 2.0 ** -24, (co, steps, err(got), err(plain))

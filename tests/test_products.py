@@ -68,3 +68,11 @@ def test_outputs_that_no_launch_holds_are_refused():
     assert linear(**big) == -5 and linear(dtype=BF16, **big) == -5
     assert mec.lib.mec_linear_workspace_bytes(1 << 30, 5, 1024, F32) == -5
     assert linear_grad(rows=1 << 30, i_c=1024, k_c=5, gp=5, xp=1024, wb=1 << 62) == -5
+
+
+def test_steps_are_paired_only_where_that_was_shown_to_be_precise():
+    """Five steps or more of the default coefficients."""
+    for batch, rows, cols in ((1, 256, 2304), (23, 2304, 256), (6, 2016, 53), (2, 32, 2160), (4, 200, 400)):
+        assert [kn.orth_pairs(batch, rows, cols, n) for n in range(1, 8)] == [False] * 4 + [True] * 3
+        for other in ((1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (4.0, -6.0, 2.5), (3.4445, -4.775, 2.03)):
+            assert not any(kn.orth_pairs(batch, rows, cols, n, other) for n in range(1, 11))
