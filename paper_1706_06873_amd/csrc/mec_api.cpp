@@ -693,6 +693,11 @@ int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, f
     return mec::orth_pairs(batch, rows, cols, steps, a, b, c);
 }
 
+int mec_internal_dword_granule(int odd, int k) {
+    const mec::DwordGranule g = mec::dword_granule(odd != 0, k);
+    return (k + g.wide) | (k + g.single) << 16;
+}
+
 int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split) {
     const mec::ProductPlan p = mec::plan_product((mec::Layout)layout, dtype, M, N, K, batch, may_split ? kMaxShares : 1);
     return p.kernel < 0 ? MEC_ERR_UNSUPPORTED : p.kernel + 16 * p.splits;

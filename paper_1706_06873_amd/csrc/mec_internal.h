@@ -238,6 +238,9 @@ extern "C" int mec_internal_dgrad_gemm(int tile, const float* G, const float* K,
 extern "C" int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split);
 // Whether an orthogonalisation takes its first and its last two steps as one.
 extern "C" int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, float b, float c);
+// Which elements of a row a granule that begins at element k is read from by dwords: the first of
+// the 8 and, 16 bits up, the single one.
+extern "C" int mec_internal_dword_granule(int odd, int k);
 // A plain product of the layer operators (mec_product.h) by one kernel: 0 the small one, from
 // 1 the tile kernels; Y's rows are dense where splits > 1 (part: splits x M x N floats).
 extern "C" int mec_internal_product(int kernel, int layout, const void* A, const void* B, void* Y, float* part, int splits,

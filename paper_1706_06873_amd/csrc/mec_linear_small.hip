@@ -244,18 +244,19 @@ constexpr int kPatch = kRun * 32 * 2;     // bytes of a wave's patch: 64 rows of
 // any boundary, but for those that the row or the reduction cuts off. Rows along the
 // reduction at odd elements go dword by dword (whole loads of 64 rows that begin inside
 // a dword: 64 x 256 <- 3239 41.7 us, so 24.2; at even elements 14.7 and 24).
-// 16 bytes as the whole dwords around them (a dword of which one half is an element's is
-// never cut by the end of a page)
-__device__ inline u32x4v load_dwords(const uint16_t* src) {
+// Elements k .. k + 7 of a row of more than 8, by whole dwords of the row's own.
+__device__ inline u32x4v load_dwords(const uint16_t* row, int32_t k) {
     struct __attribute__((packed, aligned(4))) Any {
         u32x4v v;
     };
-    const uintptr_t at = (uintptr_t)src;
-    const u32x4v w = reinterpret_cast<const Any*>(at & ~(uintptr_t)3)->v;
-    const uint32_t last = *reinterpret_cast<const uint32_t*>((at + 14) & ~(uintptr_t)3);
-    const uint32_t by = (uint32_t)(at & 2) * 8;
-    return u32x4v{__builtin_amdgcn_alignbit(w[1], w[0], by), __builtin_amdgcn_alignbit(w[2], w[1], by),
-                  __builtin_amdgcn_alignbit(w[3], w[2], by), __builtin_amdgcn_alignbit(last, w[3], by)};
+    const bool odd = ((uintptr_t)row & 2) != 0, start = odd && k == 0;  // (k is a multiple of 8)
+    const DwordGranule g = dword_granule(odd, k);
+    const u32x4v w = reinterpret_cast<const Any*>(row + (k + g.wide))->v;
+    const uint32_t one = row[k + g.single], by = odd ? 16u : 0u;
+    // what the granule is cut from: the single element before or after the others
+    const uint32_t q[5] = {start ? one << 16 : w[0], start ? w[0] : w[1], start ? w[1] : w[2], start ? w[2] : w[3], start ? w[3] : one};
+    return u32x4v{__builtin_amdgcn_alignbit(q[1], q[0], by), __builtin_amdgcn_alignbit(q[2], q[1], by),
+                  __builtin_amdgcn_alignbit(q[3], q[2], by), __builtin_amdgcn_alignbit(q[4], q[3], by)};
 }
 
 template <bool TR, bool CLEAN>
@@ -263,7 +264,7 @@ struct Turn {
     u32x4v w[4];
     // base: the tile's first row (column); r: rows (columns) there are from it on
     __device__ inline void load(const uint16_t* base, int64_t ld, int32_t r, int32_t k, int32_t k1, int lane) {
-        const bool whole = k1 % 8 == 0, odd = (((uint64_t)base >> 1 | (uint64_t)ld) & 1) != 0;  // uniform
+        const bool whole = k1 % 8 == 0, odd = (((uint64_t)base >> 1 | (uint64_t)ld) & 1) != 0 && k1 > 8;  // uniform
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (TR) {  // row k + 16 i + lane / 4, granule lane % 4 of its 32 columns
@@ -283,7 +284,7 @@ struct Turn {
                 const uint16_t* const src = base + ((lane & 31) < r ? (lane & 31) : r - 1) * ld;
                 if constexpr (CLEAN) w[i] = *reinterpret_cast<const u32x4v*>(src + (at < k1 ? at : k1 - 8));
                 else if (whole && !odd) w[i] = load_any(src + (at < k1 ? at : k1 - 8));
-                else if (whole) w[i] = load_dwords(src + (at < k1 ? at : k1 - 8));
+                else if (whole) w[i] = load_dwords(src, at < k1 ? at : k1 - 8);
                 else w[i] = load_some(src + at, k1 - at);
                 if (at >= k1) w[i] = u32x4v{0, 0, 0, 0};
             }

@@ -72,6 +72,16 @@ ProductPlan plan_pair(const ProductPlan& x, const ProductPlan& k, int dtype, int
 // A's and B's rows are whole 16-byte granules (bf16)
 bool clean_rows(Layout layout, const Product& p);
 
+// Granule k .. k + 7 of a row of more than 8 bf16 elements by whole dwords, without a byte from
+// outside the row: 16 bytes from element k + wide on, and element k + single by itself. `odd`: the
+// granule begins inside a dword.
+struct DwordGranule {
+    int32_t wide, single;
+};
+constexpr DwordGranule dword_granule(bool odd, int32_t k) {
+    return !odd ? DwordGranule{0, 7} : k == 0 ? DwordGranule{1, 0} : DwordGranule{-1, 7};
+}
+
 // Enqueue the product (dtype of A, B, Z, R, Y), with p.splits shares that leave their partial
 // sums where it is above 1. hipErrorNotSupported where there is no such kernel.
 hipError_t launch_product(const ProductPlan& plan, Layout layout, Product p, int dtype, hipStream_t stream);

@@ -217,3 +217,31 @@ def test_any_steps_and_coefficients_are_as_precise_as_plain_steps(batch, rows, c
         got = mec.orthogonalize(U.to(DEV), steps=steps, coefficients=co).cpu()
         err = lambda x: ((x.double() - want).norm() / want.norm()).item()  # noqa: E731
         assert err(got) <= 2 * err(plain) + 2.0 ** -24, (co, steps, err(got), err(plain))
+
+
+# ---------------------------------------------------------------- rows at odd elements
+
+@pytest.mark.parametrize("layout", [kn.XK, kn.XKT, kn.XTK])
+@pytest.mark.parametrize("K", [1, 7, 8, 9, 16, 24, 33, 264, 1000, 1001, 3239])
+def test_small_kernel_on_rows_at_odd_elements(layout, K):
+    """bf16 rows that begin inside a dword, every other or all of them, with NaNs around each."""
+    g = torch.Generator().manual_seed(K)
+    M, N = 37, 45
+    a, b = randn(g, M, K).to(BF16), randn(g, K, N).to(BF16)
+    want = a.double() @ b.double()
+    err = (K + 8) * 2.0 ** -23 * 1.01 * (a.double().abs() @ b.double().abs())
+
+    def placed(t, left, gap):
+        pitch = t.shape[1] + gap
+        wide = torch.full((t.shape[0] * pitch + 8,), math.nan, dtype=BF16, device=DEV)
+        view = wide.as_strided(t.shape, (pitch, 1), left)
+        view.copy_(t.to(DEV))
+        return view
+
+    at = a.T.contiguous() if layout == kn.XTK else a
+    bt = b.T.contiguous() if layout == kn.XKT else b
+    for left in (0, 1, 2, 3):
+        for odd in (0, 1):
+            gap = 2 + (K + odd) % 2
+            print("[case]", layout, K, left, gap, flush=True)
+            within(kn.product(0, layout, placed(at, left, gap), placed(bt, 3 - left, gap)), want, err, (left, gap))

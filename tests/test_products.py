@@ -76,3 +76,16 @@ def test_steps_are_paired_only_where_that_was_shown_to_be_precise():
         assert [kn.orth_pairs(batch, rows, cols, n) for n in range(1, 8)] == [False] * 4 + [True] * 3
         for other in ((1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (4.0, -6.0, 2.5), (3.4445, -4.775, 2.03)):
             assert not any(kn.orth_pairs(batch, rows, cols, n, other) for n in range(1, 11))
+
+
+@pytest.mark.parametrize("odd", [0, 1])
+def test_granules_by_dwords_stay_inside_their_row(odd):
+    """Rows of more than 8 elements from an odd or even element on: whole dwords, every element of the
+    granule, none from outside the row (the small bf16 kernel's rows at odd elements)."""
+    for K in (9, 15, 16, 24, 1001, 4096):
+        for k in range(0, K - 7, 8):
+            got = mec.lib.mec_internal_dword_granule(odd, k)
+            wide, single = got & 0xffff, got >> 16
+            read = set(range(wide, wide + 8)) | {single}
+            assert read >= set(range(k, k + 8)) and min(read) >= 0 and max(read) < K, (K, k, read)
+            assert (odd + wide) % 2 == 0
