@@ -318,7 +318,9 @@ int mec_conv2d_wgrad_noalloc(const void* I, const float* G, float* dK,
  * than a launch holds). Results are reproducible:
  * every sum has an order fixed by the sizes, the alignments, the activation and which
  * operands are given (no atomics).
- * Infinities and NaNs spread as in the formulas.
+ * Infinities and NaNs spread as in the formulas, but for act': the smooth slopes take their
+ * limits, 0 and 1, at infinities (GELU's beyond |z| = 12, where fp32 holds nothing else), and
+ * ReLU's selects G where z > 0, else 0 whatever G is.
  * ------------------------------------------------------------------------ */
 
 /* Activations: z; max(z, 0); z s(z); z s(2u), u = sqrt(2/pi) (z + 0.044715 z^3), the

@@ -251,8 +251,8 @@ hipError_t launch_sum_pairs(const float* part, int64_t count, int64_t n, float* 
     return sum_parts<float>(part, count, 2 * n, n, out, out2, stream);
 }
 
-// Shares of the rows: one up to 256 rows; else enough to fill the GPU, at least 32 rows each,
-// and partial sums that stay a small part of the traffic.
+// Shares of the rows: one up to 256 rows; else enough to fill the GPU, of about 32 rows at least
+// (257 in 9 shares of 29), and partial sums that stay a small part of the traffic.
 int32_t act_grad_shares(int64_t rows, int64_t N) {
     if (rows <= 256) return 1;
     const int64_t strips = (N + 511) / 512;

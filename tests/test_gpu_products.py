@@ -245,3 +245,47 @@ def test_small_kernel_on_rows_at_odd_elements(layout, K):
             gap = 2 + (K + odd) % 2
             print("[case]", layout, K, left, gap, flush=True)
             within(kn.product(0, layout, placed(at, left, gap), placed(bt, 3 - left, gap)), want, err, (left, gap))
+
+
+# ---------------------------------------------------------------- activations at their ends
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [7, 8, 300])
+def test_slopes_at_infinities_and_nans(dtype, width):
+    """The smooth slopes' limits, ReLU's choice, and NaN where Z is one; also that dX, dK and dbias
+    follow from the dZ that comes of it."""
+    inf, nan = math.inf, math.nan
+    z = torch.tensor([inf, -inf, nan, 20.0, -20.0, 1e30, -1e30, 0.0, -0.0])
+    rows = z.numel()
+    Z = z.view(-1, 1).expand(rows, width).contiguous()
+    G = torch.full((rows, width), 1.5)
+    limits = {"relu": [1, 0, 0, 1, 0, 1, 0, 0, 0], "silu": [1, 0, nan, 1, 0, 1, 0, 0.5, 0.5], "gelu": [1, 0, nan, 1, 0, 1, 0, 0.5, 0.5]}
+    for act, slope in limits.items():
+        print("[case]", dtype, width, act, flush=True)
+        X, K = torch.ones(rows, 3, dtype=dtype, device=DEV), torch.ones(3, width, dtype=dtype, device=DEV)
+        dX, dK, db, dZ = (t.cpu().double() for t in mec.linear_grad(G.to(dtype).to(DEV), X, K, Z.to(dtype).to(DEV), act))
+        want = 1.5 * torch.tensor(slope).double()
+        # (silu at +-20: e^-20 times 20 is 4.2e-8, and 1 minus that)
+        tol = 1.5 * 2.0 ** -24 + 1e-7 + HALF[dtype] * want.abs().nan_to_num(0.0)
+        d = dZ - want.view(-1, 1)
+        assert torch.equal(torch.isnan(dZ), torch.isnan(want).view(-1, 1).expand(rows, width))
+        assert (d.abs().nan_to_num(0.0) <= tol.view(-1, 1)).all()
+        assert torch.equal(torch.isnan(dX), torch.isnan(want).view(-1, 1).expand(rows, 3))
+        assert torch.isnan(dK).all() == torch.isnan(want).any() and torch.isnan(db).all() == torch.isnan(want).any()
+    # ReLU selects: what G is where Z is not above 0 does not matter
+    G[1], G[4] = nan, inf
+    dX, dK, db, dZ = mec.linear_grad(G.to(dtype).to(DEV), X, K, Z.to(dtype).to(DEV), "relu")
+    assert (dZ[1] == 0).all() and (dZ[4] == 0).all() and torch.isfinite(dX).all() and torch.isfinite(dK).all()
+    assert torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_activations_at_infinities_and_nans(dtype):
+    """The formulas as they are: z s(z) at -infinity is -infinity times 0."""
+    inf, nan = math.inf, math.nan
+    z = torch.tensor([[inf], [-inf], [nan], [100.0], [-100.0]]).to(dtype).to(DEV)
+    one = torch.ones(1, 1, dtype=dtype, device=DEV)
+    for act, want in (("none", [inf, -inf, nan, 100, -100]), ("relu", [inf, 0, nan, 100, 0]), ("silu", [inf, nan, nan, 100, 0]),
+                      ("gelu", [inf, nan, nan, 100, 0])):
+        got = mec.linear(z, one, act=act).cpu().float().flatten()
+        assert torch.allclose(got, torch.tensor(want, dtype=torch.float32), rtol=0, atol=1e-30, equal_nan=True), (act, got)
