@@ -11,7 +11,7 @@ import torch
 
 import kernels as kn
 import paper_1706_06873_amd as mec
-from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, close, orth64, randn, rows_of, slope64
+from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, act_error, close, orth64, randn, rows_of, slope64
 
 pytestmark = pytest.mark.gpu
 
@@ -289,3 +289,68 @@ def test_activations_at_infinities_and_nans(dtype):
                       ("gelu", [inf, nan, nan, 100, 0])):
         got = mec.linear(z, one, act=act).cpu().float().flatten()
         assert torch.allclose(got, torch.tensor(want, dtype=torch.float32), rtol=0, atol=1e-30, equal_nan=True), (act, got)
+
+
+# ---------------------------------------------------------------- epilogues
+
+EPILOGUE = [(300, 280, 96, 0), (257, 131, 64, 5), (130, 67, 77, 3), (520, 264, 40, 8), (65, 300, 128, 1), (33, 24, 200, 0)]
+
+
+@pytest.mark.parametrize("dtype,kernel", [(F32, i) for i in range(5)] + [(BF16, i) for i in range(6)])
+def test_every_kernels_epilogue(dtype, kernel):
+    """Bias, activation, residual first or last, Z, and R in Y's place, by every kernel whatever the
+    plans give it: ragged ends, unaligned pitches. The bounds are test_linear's."""
+    for n, (M, N, K, gap) in enumerate(EPILOGUE):
+        g = torch.Generator().manual_seed(M + N + K)
+        a, b = randn(g, M, K).to(dtype), (randn(g, K, N) / math.sqrt(K)).to(dtype)
+        bias, R = randn(g, N), randn(g, M, N).to(dtype)
+        A, B = rows_of(a, gap), rows_of(b, 0)
+        x, k, r = a.double(), b.double(), R.double()
+        for act, res, first, has_bias, keep in (("none", 1, 1, 1, 1), ("relu", 1, 1, 1, 1), ("silu", 1, 0, 1, 0), ("gelu", 1, 0, 0, 1),
+                                                ("gelu", 0, 0, 1, 1), ("silu", 1, 1, 0, 0), ("none", 1, 0, 1, 0)):
+            print("[case]", dtype, kernel, M, N, K, gap, act, res, first, flush=True)
+            wide = torch.full((M, N + gap), 7.0, dtype=dtype, device=DEV)
+            in_place = bool(res) and n % 2 == 1
+            if in_place:
+                wide[:, :N] = R.to(DEV)
+            Y = wide[:, :N]
+            got = kn.product_with(kernel, kn.XK, A, B, R=None if not res else Y if in_place else rows_of(R, gap),
+                                  bias=bias.to(DEV) if has_bias else None, act=act, res_first=bool(first), Z=bool(keep), Y=Y)
+            z = x @ k + bias.double() * has_bias + (r if first and res else 0)
+            err = (K + 8) * 2.0 ** -23 * (x.abs() @ k.abs() + bias.abs().double() * has_bias + r.abs() * res)
+            if keep:
+                close(got[1], z, err + HALF[dtype] * z.abs(), (kernel, act, "Z"))
+            y = act64(act, z) + (r if res and not first else 0)
+            tol = 1.13 * err + act_error(act, z, HALF[dtype]) + 2.0 ** -22 * r.abs() * res  # |act'| < 1.13
+            close(Y, y, tol + HALF[dtype] * (y.abs() + tol), (kernel, act, "Y"))
+            assert (wide[:, N:] == 7).all()
+
+
+# ---------------------------------------------------------------- fp32: all six products of the split
+
+@pytest.mark.parametrize("layout", [kn.XK, kn.XKT, kn.XTK])
+def test_fp32_products_to_fp32s_own_precision(layout):
+    """64 products a sum, in four steps that cut off at most 2^-23 of their partial sum, half of it on
+    average, and three roundings more (the parts left out, the two sums' sum, the output's place):
+    6 times 2^-24 of the whole. Leaving out any of the six products of the parts is more (shown on
+    the CPU by test_products.py)."""
+    g = torch.Generator().manual_seed(64)
+    a, b = randn(g, 300, 64), randn(g, 64, 280)
+    want = a.double() @ b.double()
+    A = (a.T.contiguous() if layout == kn.XTK else a).to(DEV)
+    B = (b.T.contiguous() if layout == kn.XKT else b).to(DEV)
+    for kernel in range(5):
+        got = kn.product(kernel, layout, A, B).cpu().double()
+        assert (got - want).norm() <= 6 * 2.0 ** -24 * want.norm(), kernel
+
+
+def test_gradients_on_a_given_stream():
+    g = torch.Generator().manual_seed(23)
+    for dt in (F32, BF16):
+        X, K, G, Z = (randn(g, *s).to(dt).to(DEV) for s in ((3000, 72), (72, 136), (3000, 136), (3000, 136)))
+        want = mec.linear_grad(G, X, K, Z, "gelu")
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        got = mec.linear_grad(G, X, K, Z, "gelu", stream=side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

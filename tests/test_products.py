@@ -89,3 +89,22 @@ def test_granules_by_dwords_stay_inside_their_row(odd):
             read = set(range(wide, wide + 8)) | {single}
             assert read >= set(range(k, k + 8)) and min(read) >= 0 and max(read) < K, (K, k, read)
             assert (odd + wide) % 2 == 0
+
+
+def test_the_fp32_bound_tells_a_lost_product_of_the_split():
+    """Values as hi + mid + lo in bf16, products of all parts but one of the six that the kernels take:
+    each loss is above the bound that the kernels are held to on 64 products a sum."""
+    g = torch.Generator().manual_seed(64)
+    a, b = torch.randn(300, 64, generator=g), torch.randn(64, 280, generator=g)
+
+    def split(x):
+        hi = x.bfloat16()
+        mid = (x - hi.float()).bfloat16()
+        return [t.double() for t in (hi, mid, (x - hi.float() - mid.float()).bfloat16())]
+    want, A, B = a.double() @ b.double(), split(a), split(b)
+    parts = [(0, 0), (1, 0), (0, 1), (1, 1), (2, 0), (0, 2)]
+    bound = 6 * 2.0 ** -24 * want.norm()
+    error = lambda keep: (sum(A[i] @ B[j] for i, j in keep) - want).norm()  # noqa: E731
+    assert error(parts) <= bound / 6
+    for lost in parts:
+        assert error([p for p in parts if p != lost]) > bound, lost
