@@ -384,6 +384,13 @@ GradPlan grad_plan(int64_t rows, int64_t i_c, int64_t k_c, int dtype, int act) {
     return g;
 }
 
+// How dX and dK are computed where both are wanted.
+enum class GradRoute { kApart = 0, kSmallPair = 1, kTilePair = 2 };
+GradRoute grad_route(const GradPlan& plan, const mec::ProductPlan& px, const mec::ProductPlan& pk, bool clean) {
+    if (px.kernel == 0 && pk.kernel == 0) return GradRoute::kSmallPair;
+    return plan.pair.kernel && clean ? GradRoute::kTilePair : GradRoute::kApart;
+}
+
 }  // namespace
 
 int mec_linear(const void* X, const void* K, const float* bias, const void* R, void* Y, void* Z, int64_t rows, int i_c,
@@ -500,10 +507,12 @@ int mec_linear_grad(const void* G, const void* X, const void* K, const void* Z, 
     x.second = k.second = low ? (int64_t)((uintptr_t)low - (uintptr_t)dZ) : 0;
     const mec::ProductPlan px = mec::refine_plan(plan.x, mec::Layout::kXKt, dtype, x);
     const mec::ProductPlan pk = mec::refine_plan(plan.k, mec::Layout::kXtK, dtype, k);
-    if (dX && dK && px.kernel == 0 && pk.kernel == 0)
+    const GradRoute route = dX && dK ? grad_route(plan, px, pk, !dtype || (mec::clean_rows(mec::Layout::kXKt, x) &&
+                                                                          mec::clean_rows(mec::Layout::kXtK, k)))
+                                     : GradRoute::kApart;
+    if (route == GradRoute::kSmallPair)
         return hip_status(mec::launch_product_small_pair(x, k, dtype, st), "gradients of the input and the kernel");
-    if (dX && dK && plan.pair.kernel &&
-        (!dtype || (mec::clean_rows(mec::Layout::kXKt, x) && mec::clean_rows(mec::Layout::kXtK, k)))) {
+    if (route == GradRoute::kTilePair) {
         k.splits = plan.pair.splits;
         rc = hip_status(dtype ? mec::launch_product_bf16_pair(x, k, st) : mec::launch_product_f32_pair(x, k, st),
                         "gradients of the input and the kernel");
@@ -691,6 +700,26 @@ int mec_internal_product_with(int kernel, int layout, int dtype, int M, int N, i
 
 int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, float b, float c) {
     return mec::orth_pairs(batch, rows, cols, steps, a, b, c);
+}
+
+int mec_internal_orth_plan(int batch, int rows, int cols, int gram) {
+    const mec::ProductPlan p = mec::orth_plan(batch, rows, cols, gram != 0);
+    return p.kernel < 0 ? MEC_ERR_UNSUPPORTED : p.kernel + 16 * p.splits;
+}
+
+int mec_internal_linear_grad_route(int rows, int i_c, int k_c, int dtype, int act) {
+    if (rows < 1 || i_c < 1 || k_c < 1 || !valid_dtype(dtype) || !valid_act(act)) return MEC_ERR_INVALID_ARG;
+    const GradPlan g = grad_plan(rows, i_c, k_c, dtype, act);
+    const bool clean = !dtype || (i_c % 8 == 0 && k_c % 8 == 0);
+    mec::Operands with;
+    with.clean = clean;
+    with.two = g.two;
+    auto refined = [&](const mec::ProductPlan& p, mec::Layout layout, int M, int N, int K) {
+        return clean ? p : mec::plan_product(layout, dtype, M, N, K, 1, p.splits, false, with);
+    };
+    const mec::ProductPlan px = refined(g.x, mec::Layout::kXKt, rows, i_c, k_c), pk = refined(g.k, mec::Layout::kXtK, i_c, k_c, rows);
+    const GradRoute route = grad_route(g, px, pk, clean);
+    return (int)route + 16 * (route == GradRoute::kTilePair ? g.pair.splits : pk.splits);
 }
 
 int mec_internal_dword_granule(int odd, int k) {

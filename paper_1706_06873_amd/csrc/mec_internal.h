@@ -238,6 +238,11 @@ extern "C" int mec_internal_dgrad_gemm(int tile, const float* G, const float* K,
 extern "C" int mec_internal_product_plan(int layout, int dtype, int M, int N, int K, int batch, int may_split);
 // Whether an orthogonalisation takes its first and its last two steps as one.
 extern "C" int mec_internal_orth_pairs(int batch, int rows, int cols, int steps, float a, float b, float c);
+// The kernel of its Gram matrices (of its m x m products), plus 16 times its shares.
+extern "C" int mec_internal_orth_plan(int batch, int rows, int cols, int gram);
+// How a backward pass on dense, aligned operands computes dX and dK: 0 in a launch each, 1 both by
+// the small kernels in one launch, 2 both by tiles in one launch; plus 16 times dK's shares.
+extern "C" int mec_internal_linear_grad_route(int rows, int i_c, int k_c, int dtype, int act);
 // Which elements of a row a granule that begins at element k is read from by dwords: the first of
 // the 8 and, 16 bits up, the single one.
 extern "C" int mec_internal_dword_granule(int odd, int k);

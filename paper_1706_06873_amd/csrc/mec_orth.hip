@@ -145,6 +145,15 @@ bool step_preferred(int64_t m, int64_t rows, int64_t cols, int32_t batch) {
     return m <= kOrthStepMax && rows <= 2048 && cols <= 2048 && ((rows + 31) / 32) * ((cols + 31) / 32) * batch <= 256;
 }
 
+// The products of a step of m = min(rows, cols): the Gram matrix, in shares if that helps, and
+// products of two m x m matrices.
+ProductPlan gram_plan(int32_t batch, int64_t rows, int64_t cols) {
+    const bool wide = rows <= cols;
+    const int64_t m = wide ? rows : cols, n = wide ? cols : rows;
+    return plan_product(wide ? Layout::kXKt : Layout::kXtK, 0, m, m, n, batch, gram_shares(m, batch), true);
+}
+ProductPlan square_plan(int32_t batch, int64_t m) { return plan_product(Layout::kXKt, 0, m, m, m, batch, 1, true); }
+
 // How the steps are taken: by products, in a launch each, or in pairs at both ends.
 enum class Steps { kSingle, kOneLaunch, kPairs };
 Steps plan_steps(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float a, float b, float c) {
@@ -157,6 +166,10 @@ Steps plan_steps(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float
 
 bool orth_pairs(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float a, float b, float c) {
     return plan_steps(batch, rows, cols, steps, a, b, c) == Steps::kPairs;
+}
+
+ProductPlan orth_plan(int32_t batch, int64_t rows, int64_t cols, bool gram) {
+    return gram ? gram_plan(batch, rows, cols) : square_plan(batch, rows < cols ? rows : cols);
 }
 
 // Two copies of X, the m x m matrices and the partial norms; the output is the second copy's
@@ -192,6 +205,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
     q.eps = eps;
     hipError_t e = dtype ? normalise<uint16_t>(q, batch, stream) : normalise<float>(q, batch, stream);
 
+    const ProductPlan grams = gram_plan(batch, rows, cols), squares = square_plan(batch, m);
     Product base{};
     base.batch = batch;
     base.splits = 1;
@@ -211,7 +225,7 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.beta = beta;
         p.diag = diag;
         p.symmetric = 1;
-        e = launch_product(Layout::kXKt, p, 0, stream);
+        e = launch_product(squares, Layout::kXKt, p, 0, stream);
     };
     int copy = 0;
     const Steps how = plan_steps(batch, rows, cols, steps, a, b, c);
@@ -232,10 +246,8 @@ hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, i
         p.y_batch = mm;
         p.symmetric = 1;
         p.part = S[1];  // the other squares are free now
-        const Layout gram = wide ? Layout::kXKt : Layout::kXtK;
-        const ProductPlan plan = plan_product(gram, 0, m, m, n, batch, shares, true);
-        e = launch_product(plan, gram, p, 0, stream);
-        if (e == hipSuccess && plan.splits > 1) e = launch_sum_parts(S[1], plan.splits, batch * mm, A, 0, stream);
+        e = launch_product(grams, wide ? Layout::kXKt : Layout::kXtK, p, 0, stream);
+        if (e == hipSuccess && grams.splits > 1) e = launch_sum_parts(S[1], grams.splits, batch * mm, A, 0, stream);
         copy ^= 1;
         void* const to = left ? static_cast<void*>(X[copy]) : O;
         if (one) {

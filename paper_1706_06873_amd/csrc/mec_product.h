@@ -130,6 +130,7 @@ hipError_t launch_norm_grad(const void* G, int64_t ldg, const void* X, int64_t l
                             int dtype, hipStream_t stream);
 
 // mec_orth.hip
+ProductPlan orth_plan(int32_t batch, int64_t rows, int64_t cols, bool gram);  // of its Gram matrices, or its squares
 bool orth_pairs(int32_t batch, int64_t rows, int64_t cols, int32_t steps, float a, float b, float c);  // steps in pairs
 int64_t orth_workspace_bytes(int32_t batch, int64_t rows, int64_t cols, int dtype);
 hipError_t launch_orth(const void* U, void* O, void* workspace, int32_t batch, int64_t rows, int64_t cols, int32_t steps,

@@ -135,3 +135,15 @@ _lib.mec_internal_orth_pairs.argtypes = [_i] * 4 + [ctypes.c_float] * 3
 def orth_pairs(batch, rows, cols, steps=5, coefficients=(3.4445, -4.7750, 2.0315)):
     """Whether an orthogonalisation takes its first and its last two steps as one."""
     return bool(_lib.mec_internal_orth_pairs(batch, rows, cols, steps, *coefficients))
+
+
+def orth_plan(batch, rows, cols, gram=True):
+    """(kernel, shares) of an orthogonalisation's Gram matrices, or of its products of two squares."""
+    r = _lib.mec_internal_orth_plan(batch, rows, cols, int(gram))
+    return r % 16, r // 16
+
+
+def linear_grad_route(rows, i_c, k_c, dtype, act="none"):
+    """(how dX and dK are computed: 0 apart, 1 a pair of small ones, 2 a pair of tiles; dK's shares)."""
+    r = _lib.mec_internal_linear_grad_route(rows, i_c, k_c, mec.F32 if dtype == "f32" else mec.BF16, mec._ACTS[act])
+    return r % 16, r // 16

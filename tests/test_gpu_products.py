@@ -11,7 +11,7 @@ import torch
 
 import kernels as kn
 import paper_1706_06873_amd as mec
-from test_gpu_layers import BF16, C0, DEV, F32, HALF, act64, act_error, close, orth64, randn, rows_of, slope64
+from test_gpu_layers import BF16, C0, DEV, F32, HALF, ORTH_TOL, act64, act_error, close, orth64, randn, rows_of, slope64
 
 pytestmark = pytest.mark.gpu
 
@@ -326,6 +326,57 @@ def test_every_kernels_epilogue(dtype, kernel):
             assert (wide[:, N:] == 7).all()
 
 
+# ---------------------------------------------------------------- symmetric products
+
+@pytest.mark.parametrize("kernel", range(5))
+@pytest.mark.parametrize("layout", [kn.XKT, kn.XTK])
+def test_symmetric_products_and_their_mirror_images(kernel, layout):
+    """X X^T of one and of several tiles, ragged, by every fp32 kernel: alpha X X^T + beta R + diag I with
+    R symmetric, stacks, and shares of the reduction (which leave the sum alone)."""
+    for M, K, batch, splits in ((64, 100, 1, 1), (65, 72, 3, 1), (200, 130, 2, 1), (321, 96, 1, 1), (130, 1000, 1, 3),
+                                (200, 700, 2, 2), (256, 64, 2, 1)):
+        if splits > 1 and kernel == 0:
+            continue
+        g = torch.Generator().manual_seed(M + K + batch)
+        a = randn(g, batch, M, K)
+        R = randn(g, batch, M, M)
+        R = R + R.mT
+        want, err = a.double() @ a.double().mT, (K + 8) * 2.0 ** -23 * (a.double().abs() @ a.double().abs().mT)
+        X = (a if layout == kn.XKT else a.mT.contiguous()).to(DEV)
+        X, Rd = (X[0], R[0].to(DEV)) if batch == 1 else (X, R.to(DEV))
+        print("[case]", kernel, layout, M, K, batch, splits, flush=True)
+        Y = kn.product_with(kernel, layout, X, X, splits, symmetric=True, batch=batch)
+        close(Y.reshape(want.shape), want, err + 2.0 ** -23 * want.abs(), (kernel, "plain"))
+        if splits == 1:
+            Y = kn.product_with(kernel, layout, X, X, symmetric=True, batch=batch, R=Rd, alpha=2.0315, beta=-4.775, diag=3.4445)
+            full = 2.0315 * want - 4.775 * R.double() + 3.4445 * torch.eye(M).double()
+            tol = 2.04 * err + 2.0 ** -22 * (2.04 * want.abs() + 4.78 * R.double().abs() + 3.5)
+            close(Y.reshape(want.shape), full, tol, (kernel, "with R"))
+
+
+@pytest.mark.parametrize("batch,rows,cols,gram,square", [
+    (23, 2304, 256, (4, 1), (3, 1)),    # three groups of waves, and tiles with their mirror images
+    (4, 321, 330, (3, 1), (3, 1)),      # ragged
+    (8, 150, 4000, (3, 13), (0, 1)),    # shares of several ragged tiles
+    (40, 100, 2000, (3, 6), (3, 1)),
+    (1, 72, 20000, (4, 27), (0, 1)),    # shares of the three groups' tiles
+    (60, 200, 230, (3, 1), (3, 1)),
+    (1, 700, 900, (3, 3), (0, 1)),
+])
+def test_orthogonalize_by_symmetric_products(batch, rows, cols, gram, square):
+    """Stacks and single matrices whose Gram matrices and squares are computed by halves."""
+    assert kn.orth_plan(batch, rows, cols) == gram and kn.orth_plan(batch, rows, cols, gram=False) == square
+    g = torch.Generator().manual_seed(rows * 3 + cols)
+    few = min(batch, 4)  # as many different ones; the others are copies of these
+    U = 1e-3 * (randn(g, few, rows, cols) + 3 * randn(g, few, rows, 1) * randn(g, few, 1, cols))
+    print("[case]", batch, rows, cols, flush=True)
+    O = mec.orthogonalize(U[torch.arange(batch) % few].to(DEV)).cpu()
+    want = orth64(U)
+    for i in range(batch):
+        err = (O[i].double() - want[i % few]).norm() / want[i % few].norm()
+        assert err <= ORTH_TOL, (i, float(err))
+
+
 # ---------------------------------------------------------------- fp32: all six products of the split
 
 @pytest.mark.parametrize("layout", [kn.XK, kn.XKT, kn.XTK])
@@ -342,6 +393,38 @@ def test_fp32_products_to_fp32s_own_precision(layout):
     for kernel in range(5):
         got = kn.product(kernel, layout, A, B).cpu().double()
         assert (got - want).norm() <= 6 * 2.0 ** -24 * want.norm(), kernel
+
+
+# ---------------------------------------------------------------- dX and dK in one launch
+
+@pytest.mark.parametrize("dtype,rows,i_c,k_c,act,route", [
+    ("f32", 1000, 1000, 1000, "none", (2, 1)), ("f32", 2000, 300, 301, "silu", (2, 7)), ("f32", 900, 520, 520, "gelu", (2, 2)),
+    ("f32", 1134, 374, 112, "none", (2, 4)), ("f32", 700, 130, 1001, "gelu", (1, 1)), ("f32", 40, 72, 48, "relu", (1, 1)),
+    ("bf16", 1200, 520, 1032, "none", (2, 1)), ("bf16", 2000, 296, 304, "gelu", (2, 7)), ("bf16", 900, 520, 520, "none", (2, 1)),
+    ("bf16", 900, 520, 520, "silu", (2, 2)), ("bf16", 40, 72, 48, "gelu", (2, 1)), ("bf16", 700, 130, 1001, "gelu", (1, 1)),
+    ("bf16", 700, 130, 1001, "none", (1, 1)),
+])
+def test_gradients_of_two_products_in_one_launch(dtype, rows, i_c, k_c, act, route):
+    assert kn.linear_grad_route(rows, i_c, k_c, dtype, act) == route
+    dt = F32 if dtype == "f32" else BF16
+    g = torch.Generator().manual_seed(rows + k_c)
+    X, K = randn(g, rows, i_c).to(dt), (randn(g, i_c, k_c) / math.sqrt(i_c)).to(dt)
+    G, Z = randn(g, rows, k_c).to(dt), (2 * randn(g, rows, k_c)).to(dt)
+    print("[case]", dtype, rows, i_c, k_c, act, flush=True)
+    dX, dK, _, dZ = mec.linear_grad(G.to(DEV), X.to(DEV), K.to(DEV), Z.to(DEV), act)
+    x, k = X.double(), K.double()
+    dz = G.double() * slope64(act, Z.double())
+    two = 2 if dt is BF16 and act in ("silu", "gelu") else 1
+    # the slope's evaluation, and (bf16) what is left over of two roundings
+    ez = 0 * dz if act in ("none", "relu") else G.double().abs() * (2.0 ** -15 if dt is BF16 else 2.0 ** -18) + dz.abs() * 2.0 ** -16 * (two - 1)
+    ez = ez + (2.0 ** -24 * dz.abs() if dt is F32 else 0)
+    for got, want, bound, n, what in ((dX, dz @ k.T, dz.abs() @ k.abs().T, k_c, "dX"), (dK, x.T @ dz, x.abs().T @ dz.abs(), rows, "dK")):
+        spread = ez @ k.abs().T if what == "dX" else x.abs().T @ ez
+        err = (two * n + 8) * 2.0 ** -23 * bound + 1.01 * spread
+        close(got, want, err + HALF[dt] * (want.abs() + err), what)
+        # and each alone, by its own launch: the same but for the order of the sums
+        alone = mec.linear_grad(G.to(DEV), X.to(DEV), K.to(DEV), Z.to(DEV), act, needs=(what == "dX", what == "dK", False))[what == "dK"]
+        close(alone, want, err + HALF[dt] * (want.abs() + err), what + " alone")
 
 
 def test_gradients_on_a_given_stream():
