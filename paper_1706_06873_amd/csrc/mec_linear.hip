@@ -327,19 +327,29 @@ __device__ inline void product_bf16(const Product& p, uint32_t b, char* lds) {
         }
     }
     if constexpr (C::kGrad) {
-        if (two) {
-            const uint16_t* const A = static_cast<const uint16_t*>(p.A) + k0 * (C::kAT ? p.lda : 1);
-            const uint16_t* const B = static_cast<const uint16_t*>(p.B) + k0 * (C::kBT ? p.ldb : 1);
+        bool odd = false;
+        if (two)
 #pragma unroll
             for (int i = 0; i < BM; ++i)
 #pragma unroll
-                for (int j = 0; j < BN; ++j) {
-                    int32_t m = m0 + (wm * BM + i) * 32 + (lane & 31), n = n0 + (wn * BN + j) * 32 + (lane & 31);
-                    m = m < p.M ? m : p.M - 1;
-                    n = n < p.N ? n : p.N - 1;
-                    finite_or_first(acc[i][j], A + m * (C::kAT ? 1 : p.lda), C::kAT ? p.lda : 1, B + n * (C::kBT ? 1 : p.ldb),
-                                    C::kBT ? p.ldb : 1, (int32_t)(k1 - k0), lane);
-                }
+                for (int j = 0; j < BN; ++j) odd |= not_finite(acc[i][j]);
+        if (odd) {
+            const int64_t ars = C::kAT ? 1 : p.lda, aks = C::kAT ? p.lda : 1, brs = C::kBT ? 1 : p.ldb, bks = C::kBT ? p.ldb : 1;
+            const int32_t len = (int32_t)(k1 - k0);
+            auto row = [&](int i) {
+                const int32_t m = m0 + (wm * BM + i) * 32 + (lane & 31);
+                return static_cast<const uint16_t*>(p.A) + k0 * aks + (m < p.M ? m : p.M - 1) * ars;
+            };
+            auto column = [&](int j) {
+                const int32_t n = n0 + (wn * BN + j) * 32 + (lane & 31);
+                return static_cast<const uint16_t*>(p.B) + k0 * bks + (n < p.N ? n : p.N - 1) * brs;
+            };
+#pragma unroll
+            for (int o = 0; o < (C::kAT ? BM : BN); ++o)
+                if (holds_infinity(C::kAT ? row(o) : column(o), C::kAT ? aks : bks, len, lane))
+#pragma unroll
+                    for (int q = 0; q < (C::kAT ? BN : BM); ++q)
+                        take_again(acc[C::kAT ? o : q][C::kAT ? q : o], row(C::kAT ? o : q), aks, column(C::kAT ? q : o), bks, len, lane);
         }
     }
     __syncthreads();

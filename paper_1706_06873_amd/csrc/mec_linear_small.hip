@@ -364,11 +364,14 @@ __device__ inline void small_bf16(const Product& p, uint32_t b0, char* lds) {
                 __builtin_amdgcn_wave_barrier();
             }
         }
-        if (second) {
+        if (second && not_finite(acc)) {
             const int32_t m = (lane & 31) < p.M - t.m0 ? (lane & 31) : p.M - t.m0 - 1;
             const int32_t n = (lane & 31) < p.N - t.n0 ? (lane & 31) : p.N - t.n0 - 1;
-            finite_or_first(acc, a + m * (AT ? 1 : p.lda) + t.k.k0 * (AT ? p.lda : 1), AT ? p.lda : 1,
-                            b + n * (BT ? 1 : p.ldb) + t.k.k0 * (BT ? p.ldb : 1), BT ? p.ldb : 1, t.k.k1 - t.k.k0, lane);
+            const int64_t aks = AT ? p.lda : 1, bks = BT ? p.ldb : 1;
+            const uint16_t* const row = a + m * (AT ? 1 : p.lda) + t.k.k0 * aks;
+            const uint16_t* const column = b + n * (BT ? 1 : p.ldb) + t.k.k0 * bks;
+            if (holds_infinity(AT ? row : column, AT ? aks : bks, t.k.k1 - t.k.k0, lane))
+                take_again(acc, row, aks, column, bks, t.k.k1 - t.k.k0, lane);
         }
     }
     __syncthreads();
