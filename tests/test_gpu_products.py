@@ -437,3 +437,40 @@ def test_gradients_on_a_given_stream():
         got = mec.linear_grad(G, X, K, Z, "gelu", stream=side)
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("layout", [kn.XKT, kn.XTK])
+def test_every_kernel_on_two_parts_and_infinities(layout):
+    """Infinities in the operand that dZ is multiplied with, infinities and NaNs in dZ, and dZ of 0: by
+    every kernel as the formula has them, the finite sums as before."""
+    for M, N, K, gap, splits in PARTS:
+        g = torch.Generator().manual_seed(M * 3 + N + K)
+        order = -1 if K % 2 else 1
+        dz, other = (randn(g, M, K), randn(g, K, N)) if layout == kn.XKT else (randn(g, K, N), randn(g, M, K))
+        r, c = dz.shape
+        dz[0, c // 2], dz[r - 1, 0], dz[r // 2, 1] = math.inf, math.nan, 0.0
+        r, c = other.shape
+        other[r - 1, c - 1], other[0, c // 3], other[r // 2, 1] = math.inf, -math.inf, math.nan
+        other = other.to(BF16)
+        first = dz.to(BF16)
+        second = torch.where(torch.isfinite(first), dz - first.float(), torch.zeros(())).to(BF16)
+        both = torch.full((2, dz.shape[0], dz.shape[1] + gap), 7.0, dtype=BF16, device=DEV)
+        at = (0, 1) if order > 0 else (1, 0)
+        both[at[0], :, :dz.shape[1]], both[at[1], :, :dz.shape[1]] = first.to(DEV), second.to(DEV)
+        Z, jump = both[at[0], :, :dz.shape[1]], order * both.stride(0) * 2
+        placed = rows_of(other.T.contiguous(), gap)
+        A, B = (Z, placed) if layout == kn.XKT else (placed, Z)
+        product = lambda z, o: z @ o if layout == kn.XKT else o @ z  # noqa: E731
+        want = product(first.double(), other.double())
+        ok = torch.isfinite(want)
+        finite = lambda t: torch.nan_to_num(t.double(), 0.0, 0.0, 0.0)  # noqa: E731
+        exact = product(finite(first) + finite(second), finite(other))
+        err = (2 * K + 8) * 2.0 ** -23 * 1.01 * product(finite(first).abs(), finite(other).abs())
+        for kernel in range(6):
+            if splits > 1 and kernel == 0:
+                continue
+            print("[case]", layout, M, N, K, gap, splits, kernel, flush=True)
+            Y = kn.product_with(kernel, layout, A, B, splits, second=jump).cpu()
+            for same in (torch.isnan, torch.isposinf, torch.isneginf):
+                assert torch.equal(same(Y), same(want)), (kernel, same)
+            within(Y[ok], exact[ok], err[ok], kernel)
