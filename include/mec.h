@@ -311,7 +311,7 @@ int mec_conv2d_wgrad_noalloc(const void* I, const float* G, float* dK,
  * same activations and the same K. An n-h-w-c tensor is `rows` pixels (i_n*h*w)
  * of its channels; consecutive pixels are `pitch` elements apart (the channel
  * count, or more where the rows are a slice of a wider tensor's channels).
- * `dtype` is the type of the activations, their gradients, K and dK; bias,
+ * Sizes are 1 at least. `dtype` is the type of the activations, their gradients, K and dK; bias,
  * gamma, beta, their gradients and the row statistics are fp32, and so is
  * everything between: each output is rounded once. Widths and pitches go up to
  * 2^20, rows to 2^30 (MEC_ERR_UNSUPPORTED beyond, and for outputs of terabytes, more tiles

@@ -477,8 +477,9 @@ def conv2d_wgrad_noalloc(I, G, k_h, k_w, s_h=1, s_w=1, dK=None, stream=None):
 # Activations are tensors with the channels last: contiguous, or 2-D (rows x channels) with
 # a row pitch, as a slice of a wider tensor's channels has. They, their gradients, K and dK
 # are float32 or bfloat16, all the same; bias, gamma, beta, their gradients and the row
-# statistics are float32. The *_workspace_bytes functions are functions of the sizes alone and
-# remember their values (0.5 us of a call).
+# statistics are float32. No size is 0. Given outputs share no memory with each other or with the
+# inputs, except where a function says that one may. The *_workspace_bytes functions are functions
+# of their arguments alone and remember their values (0.5 us of a call).
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _F32 = torch.float32
@@ -678,7 +679,8 @@ def linear_grad(G, X, K, Z=None, act="none", needs=(True, True, True), dZ=None, 
     others come back as None (X may be None without dK). dZ, the gradient of act's argument, is G
     itself with act "none"; the residual's gradient is dZ where it was added first, else G.
     dK has K's dtype and shape, dbias is float32; none of the three is computed from dZ as rounded
-    to bfloat16. A given workspace holds at least linear_grad_workspace_bytes bytes."""
+    to bfloat16. A given workspace holds at least linear_grad_workspace_bytes bytes. dZ may
+    be Z's memory, or a dense G's."""
     if stream is not None:
         return _on(stream, linear_grad, G, X, K, Z, act, needs, dZ, dX, dK, dbias, workspace)
     gs, rows, k_c, dt = _channels(G, "G")

@@ -3,7 +3,7 @@
 //   X <- (a I + b A + c A^2) X    (rows <= cols, A = X X^T; else A = X^T X, from the right),
 // all in fp32 (mec_linear_f32.hip): an error of one product grows by the factor a = 3.4 per
 // step in the directions of small singular values, 140 times over the steps after the
-// first, which fp32 has room for and bf16 (2^-9 a rounding) has not.
+// first, which fp32 has room for and bf16 (2^-8 a rounding) has not.
 //
 // Two steps at once: with P = a I + b A + c A^2 the Gram matrix after the step is P A P, so a
 // pair of steps needs one Gram matrix of X and one product with X, for P' P, and the rest on
